@@ -76,7 +76,8 @@ typedef enum mas_status {
   MAS_ERR_WORKSPACE = 3,    /* workspace NULL, misaligned or too small */
   MAS_ERR_HIP = 4,          /* a HIP runtime call or kernel launch failed */
   MAS_ERR_SCRATCH = 5,      /* mas_forward_static: the batch needs more than MAS_STATIC_SCRATCH_BYTES */
-  MAS_ERR_BAD_VALUE = 6     /* mas_forward_sentinel: the sentinel is not a finite negative number */
+  MAS_ERR_BAD_VALUE = 6     /* mas_forward_sentinel: the sentinel is not a finite negative number; a value that the call's
+                             description rules out */
 } mas_status;
 
 /* Per-item status codes written to item_status_out[b]. */
@@ -254,6 +255,175 @@ mas_status mas_forward(const float* value, const int32_t* t_x, const int32_t* t_
 mas_status mas_forward_static(const float* value, const int32_t* t_x, const int32_t* t_y,
                               uint8_t* path_out, int32_t B, int32_t T, int32_t S,
                               float* score_out, int32_t* item_status_out, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Operators around the alignment: what a text encoder that produces mu and
+ * log_sigma is made of, and the loss it is trained with.  The conventions
+ * above hold (device pointers, work enqueued on `stream` only, the caller's
+ * buffers, host-side checks before anything is enqueued), except that tensors
+ * of heads have strides and one of three element types.
+ */
+
+/* Element types of tensors of heads. */
+typedef enum mas_dtype { MAS_F32 = 0, MAS_F16 = 1, MAS_BF16 = 2 } mas_dtype;
+
+/*
+ * A tensor of heads [B, T, H, D]: strides in elements of an item, a token and
+ * a head (any values whose addresses stay in the tensor; 0 repeats an input);
+ * the D channels of a head are contiguous.  16-byte accesses are used where
+ * every head of every tensor of the call starts on a 16-byte boundary and D
+ * elements are whole 16-byte pieces; else element accesses (slower).
+ */
+typedef struct mas_heads {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} mas_heads;
+
+/*
+ * Attention of t_q[b] queries over t_k[b] keys.
+ *   q, out [B, Tq, Hq, D]; k, v [B, Tk, Hk, D]; Hq a multiple of Hk: query
+ *   head h reads key head h / (Hq / Hk).  1 <= D <= 128.
+ *   s = scale * q.k;  with cap > 0: s = cap * tanh(s / cap);  with slope:
+ *   s -= slope[h] * |place of q - place of k|;
+ *   out = sum over the keys the query sees of softmax(s) v.
+ * Places: key j is at j, query i at i + t_k - t_q: queries are the last t_q
+ * tokens of the t_k (a step over a cache; the same tokens where the lengths
+ * are equal).
+ * What a query sees: the keys j < t_k of its document (doc_start; else all),
+ * with `causal` only those up to its own place or inside its document's
+ * prefix.
+ *   t_q, t_k [B] int32 (nullable: Tq, Tk), taken as 0 below 0 and as Tq, Tk
+ *   above.  slope [Hq] fp32 (nullable).  doc_start [B, N+1] int32 (nullable):
+ *   document n holds the places [doc_start[n], doc_start[n+1]), non-decreasing
+ *   as in a row_start table; a place in no document sees nothing and is not
+ *   seen.  prefix [B, N] int32 (nullable; N = 1, the whole item, without
+ *   doc_start; needs `causal`): the first tokens of a document that all of
+ *   its tokens see.  Another table than a non-decreasing one cannot make the
+ *   kernels access memory outside the tensors, but results are unspecified.
+ * A query that sees no key (and every query past t_q) gets zeros, log-sum-exp
+ * -inf and no gradient.  Padding of the inputs never influences a result,
+ * whatever it holds.
+ * Precision: sums, maxima and totals in fp32; in the 16-bit types p and ds are
+ * rounded to the type before they are multiplied (fp16: as for its gradients
+ * at large, values below 6e-8 are lost, so scale the loss); results are
+ * rounded once.  MAS_F32 multiplies in fp32.  Repeated calls give identical
+ * bits.
+ */
+typedef struct mas_attention_desc {
+  int32_t B, Tq, Tk, Hq, Hk, D;
+  int32_t dtype;   /* mas_dtype of every tensor of heads */
+  int32_t causal;  /* 0 or 1 */
+  int32_t N;       /* documents an item (doc_start, prefix) */
+  float scale;     /* finite */
+  float cap;       /* 0: none */
+  const int32_t* t_q;
+  const int32_t* t_k;
+  const float* slope;
+  const int32_t* doc_start;
+  const int32_t* prefix;
+} mas_attention_desc;
+
+/* Bytes of device workspace for mas_attention and, with `backward`, for
+ * mas_attention_backward of this shape too; 0 for an invalid one.  256-byte
+ * aligned, no initialisation, one call at a time. */
+size_t mas_attention_workspace_bytes(const mas_attention_desc* desc, int32_t backward);
+
+/*
+ * out, fully overwritten, and lse_out [B, Hq, Tq] fp32 (nullable; what the
+ * backward pass takes): the natural log of the sum of exp(s) of the keys seen.
+ * Few rows (Tq * Hq / Hk) over long keys are split over the keys and joined.
+ * Errors: MAS_ERR_NULL_POINTER; MAS_ERR_BAD_SHAPE (extents < 1, D, Hq, N, or
+ * more than 2^22 blocks of 32 rows or keys over all items and heads);
+ * MAS_ERR_BAD_VALUE (dtype, scale, cap, prefix without causal, a tensor that
+ * does not start on an element); MAS_ERR_WORKSPACE.
+ */
+mas_status mas_attention(const mas_attention_desc* desc, const mas_heads* q, const mas_heads* k, const mas_heads* v,
+                         const mas_heads* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/*
+ * Gradients dq, dk, dv of a function whose gradient by `out` is dout, from the
+ * inputs, out and lse of mas_attention with the same desc; all fully
+ * overwritten, zeros in padding.  dk, dv of a key head are the sums over its
+ * query heads.  slope is a constant (no gradient).  No atomics.
+ */
+mas_status mas_attention_backward(const mas_attention_desc* desc, const mas_heads* dout, const mas_heads* q,
+                                  const mas_heads* k, const mas_heads* v, const mas_heads* out, const float* lse,
+                                  const mas_heads* dq, const mas_heads* dk, const mas_heads* dv, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Norm of queries and keys for each head, and their rotation by position, in
+ * one pass: x of D channels becomes y = x / sqrt(mean(x^2) + eps) * w, and of
+ * its first R channels the pairs (a, b) become (a c - b s, b c + a s) with
+ * c = cos[pos][n], s = sin[pos][n] of pair n.  Pair n is the channels
+ * (n, n + R/2), or with `interleaved` (2n, 2n+1).
+ *   q [B, T, Hq, D], k [B, T, Hk, D] (Hk = 0: queries only, k ignored).
+ *   1 <= D <= 256, R even, 0 <= R <= D.  wq, wk [D] fp32 (nullable: 1).
+ *   cos, sin [P, R/2] fp32 (nullable with R = 0).  pos [B, T] int32 (nullable:
+ *   token t is at position t); a position outside [0, P) takes the nearest row
+ *   of the tables.  t_x [B] int32 (nullable: T): tokens at t >= t_x are padding,
+ *   written as zeros.  B * T <= 2^24.
+ * Sums and products in fp32, rounded once.
+ */
+typedef struct mas_qk_desc {
+  int32_t B, T, Hq, Hk, D, R, P;
+  int32_t dtype;        /* mas_dtype of every tensor of heads */
+  int32_t interleaved;  /* 0 or 1 */
+  float eps;            /* finite, not negative */
+  const float* wq;
+  const float* wk;
+  const float* cos;
+  const float* sin;
+  const int32_t* pos;
+  const int32_t* t_x;
+} mas_qk_desc;
+
+/* q_out, k_out may be q, k themselves (same strides). */
+mas_status mas_qk_norm_rope(const mas_qk_desc* desc, const mas_heads* q, const mas_heads* k, const mas_heads* q_out,
+                            const mas_heads* k_out, hipStream_t stream);
+
+/* Bytes of device workspace for mas_qk_norm_rope_backward (256-byte aligned,
+ * no initialisation); 0 for invalid shapes. */
+size_t mas_qk_norm_rope_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hk, int32_t D);
+
+/*
+ * Gradients by q, k and the weights, from those by q_out, k_out (dq_out,
+ * dk_out) and the inputs of the forward call.  dq, dk fully overwritten, zeros
+ * in padding (they may be dq_out, dk_out themselves); dwq, dwk [D] fp32
+ * (nullable) are sums over all tokens and heads, in a fixed order.
+ */
+mas_status mas_qk_norm_rope_backward(const mas_qk_desc* desc, const mas_heads* dq_out, const mas_heads* dk_out,
+                                     const mas_heads* q, const mas_heads* k, const mas_heads* dq, const mas_heads* dk,
+                                     float* dwq, float* dwk, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+
+/*
+ * Aligned loss, and its gradients in the same pass: the negative
+ * log-likelihood of the frames under the text rows that the alignment gives
+ * them,
+ *   loss_out[b] = - sum over frames j and their rows i of value[b][i][j]
+ * with mas_loglik's value, and the gradients of
+ *   sum over b of item_weight[b] * loss_out[b]  (item_weight nullable: 1)
+ * by mu, log_sigma and z.
+ *   mu, log_sigma [B, T, D] (log_sigma nullable: sigma = 1), z [B, S, D],
+ *   row_start [B, T+1] as mas_search writes it, item_weight, loss_out [B],
+ *   dmu_out, dlog_sigma_out [B, T, D], dz_out [B, S, D] (each nullable), fp32
+ *   or int32, contiguous.  Outputs are fully overwritten: rows without a frame
+ *   and frames without a row get zeros, an item without an alignment loss 0.
+ *   1 <= D <= 65536; B * (T + 1) and B * ceil(S / 16) * ceil(D / 64) at most
+ *   2^22.  A table that is not monotone cannot make the kernels access memory
+ *   outside these tensors, but results are then unspecified.
+ * fp32 sums in a fixed order: repeated calls give identical bits.
+ */
+mas_status mas_align_loss(const float* mu, const float* log_sigma, const float* z, const int32_t* row_start,
+                          const float* item_weight, int32_t B, int32_t T, int32_t S, int32_t D, float* loss_out,
+                          float* dmu_out, float* dlog_sigma_out, float* dz_out, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace for mas_align_loss (256-byte aligned, no
+ * initialisation); 0 for invalid shapes. */
+size_t mas_align_loss_workspace_bytes(int32_t B, int32_t T, int32_t S, int32_t D);
 
 /* Human-readable name of a status code (static storage). */
 const char* mas_status_string(mas_status status);

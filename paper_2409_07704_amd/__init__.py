@@ -16,6 +16,11 @@ from ._native import (  # noqa: F401
     MasError,
     Workspace,
     lib,
+    mas_align_loss,
+    mas_align_loss_workspace_bytes,
+    mas_attention,
+    mas_attention_backward,
+    mas_attention_workspace_bytes,
     mas_expand_path,
     mas_expand_text,
     mas_forward,
@@ -23,6 +28,9 @@ from ._native import (  # noqa: F401
     mas_forward_sentinel,
     mas_forward_static,
     mas_loglik,
+    mas_qk_norm_rope,
+    mas_qk_norm_rope_backward,
+    mas_qk_norm_rope_workspace_bytes,
     mas_search,
     mas_status_string,
     mas_version,

@@ -8,7 +8,9 @@ built the binding raises instead of computing anything another way.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import math
 import os
 
 import torch
@@ -23,7 +25,30 @@ STATIC_SCRATCH_BYTES = 80 << 20  # MAS_STATIC_SCRATCH_BYTES
 ITEM_OK, ITEM_EMPTY, ITEM_INFEASIBLE, ITEM_OUT_OF_RANGE, ITEM_SYNC_TIMEOUT, ITEM_BAD_WORKSPACE = 0, 1, 2, 3, 4, 5
 
 # Every function declared in include/mas.h, with its ctypes signature.
-_P, _I32, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+_P, _I32, _I64, _SZ, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+
+
+class Heads(ctypes.Structure):
+    """mas_heads"""
+
+    _fields_ = [("data", _P), ("stride_b", _I64), ("stride_t", _I64), ("stride_h", _I64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    """mas_attention_desc"""
+
+    _fields_ = [(n, _I32) for n in ("B", "Tq", "Tk", "Hq", "Hk", "D", "dtype", "causal", "N")] + [
+        ("scale", _F), ("cap", _F)] + [(n, _P) for n in ("t_q", "t_k", "slope", "doc_start", "prefix")]
+
+
+class QkDesc(ctypes.Structure):
+    """mas_qk_desc"""
+
+    _fields_ = [(n, _I32) for n in ("B", "T", "Hq", "Hk", "D", "R", "P", "dtype", "interleaved")] + [
+        ("eps", _F)] + [(n, _P) for n in ("wq", "wk", "cos", "sin", "pos", "t_x")]
+
+
+_H, _A, _Q = ctypes.POINTER(Heads), ctypes.POINTER(AttentionDesc), ctypes.POINTER(QkDesc)
 SIGNATURES = {
     "mas_workspace_bytes": ([_I32, _I32, _I32], _SZ),
     "mas_workspace_init": ([_P, _SZ, _P], ctypes.c_int),
@@ -35,6 +60,14 @@ SIGNATURES = {
     "mas_forward_sentinel": ([_P, _P, _P, _P, _I32, _I32, _I32, ctypes.c_float, _P, _P, _P, _SZ, _P], ctypes.c_int),
     "mas_forward": ([_P, _P, _P, _P, _I32, _I32, _I32, _P], ctypes.c_int),
     "mas_forward_static": ([_P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P], ctypes.c_int),
+    "mas_attention_workspace_bytes": ([_A, _I32], _SZ),
+    "mas_attention": ([_A, _H, _H, _H, _H, _P, _P, _SZ, _P], ctypes.c_int),
+    "mas_attention_backward": ([_A, _H, _H, _H, _H, _H, _P, _H, _H, _H, _P, _SZ, _P], ctypes.c_int),
+    "mas_qk_norm_rope": ([_Q, _H, _H, _H, _H, _P], ctypes.c_int),
+    "mas_qk_norm_rope_workspace_bytes": ([_I32, _I32, _I32, _I32, _I32], _SZ),
+    "mas_qk_norm_rope_backward": ([_Q, _H, _H, _H, _H, _H, _H, _P, _P, _P, _SZ, _P], ctypes.c_int),
+    "mas_align_loss": ([_P, _P, _P, _P, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _P, _SZ, _P], ctypes.c_int),
+    "mas_align_loss_workspace_bytes": ([_I32, _I32, _I32, _I32], _SZ),
     "mas_status_string": ([ctypes.c_int], ctypes.c_char_p),
     "mas_version": ([], ctypes.c_int),
 }
@@ -265,3 +298,230 @@ def mas_forward(value, t_x, t_y, path_out=None, stream=None):
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     _check("mas_forward", lib().mas_forward(pv, px, py, pp, B, T, S, _stream(stream, value.device)))
     return path_out
+
+
+# ------------------------------------------------ operators around the alignment
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _heads(t, name, like=None, shape=None):
+    """mas_heads of a tensor [B, T, H, D] with contiguous channels."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device (cuda/hip) tensor")
+    if t.dtype not in _DTYPES or (like is not None and t.dtype != like.dtype):
+        raise TypeError(f"{name} must be {like.dtype if like is not None else 'float32, float16 or bfloat16'}, got {t.dtype}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [B, T, H, D]")
+    if shape is not None and t.shape != torch.Size(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return Heads(t.data_ptr(), sb, st, sh)
+
+
+def _arg(t, name, dtype, shape, device):
+    """Pointer of an optional contiguous tensor on the call's device."""
+    p = _dev_ptr(t, name, dtype, shape)
+    if t is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    return p
+
+
+def _on(stream, device):
+    """The call's stream as a context in which to allocate: memory the call
+    brings along belongs to the stream that uses it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = _stream(stream, device)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _scratch(workspace, nbytes, device, stream):
+    """(pointer, bytes) of the caller's uint8 workspace, or of a new one, and what
+    keeps it alive until the call is enqueued."""
+    if nbytes == 0:
+        raise ValueError("invalid shape")
+    if workspace is None:
+        with _on(stream, device):
+            workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        off = -workspace.data_ptr() % 256
+        return workspace.data_ptr() + off, nbytes, workspace
+    return _arg(workspace, "workspace", torch.uint8, None, device), workspace.numel(), workspace
+
+
+def _empty(shape, dtype, device, stream):
+    with _on(stream, device):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q must be [B, Tq, Hq, D] and k [B, Tk, Hk, D]")
+    B, Tq, Hq, D = q.shape
+    Tk, Hk = k.shape[1], k.shape[2]
+    dev = q.device
+    N = 1
+    if doc_start is not None:
+        if doc_start.dim() != 2:
+            raise ValueError("doc_start must be [B, N + 1]")
+        N = doc_start.shape[1] - 1
+    return AttentionDesc(B, Tq, Tk, Hq, Hk, D, _DTYPES.get(q.dtype, -1), 1 if causal else 0, N,
+                         1.0 / math.sqrt(max(D, 1)) if scale is None else scale, cap,
+                         _arg(t_q, "t_q", torch.int32, (B,), dev), _arg(t_k, "t_k", torch.int32, (B,), dev),
+                         _arg(slope, "slope", torch.float32, (Hq,), dev),
+                         _arg(doc_start, "doc_start", torch.int32, (B, N + 1), dev),
+                         _arg(prefix, "prefix", torch.int32, (B, N), dev))
+
+
+def mas_attention_workspace_bytes(q, k, backward: bool = False) -> int:
+    """Bytes of workspace for mas_attention of q [B, Tq, Hq, D] over k [B, Tk,
+    Hk, D] and, with `backward`, for mas_attention_backward too."""
+    d = _attention_desc(q, k, None, None, False, None, 0.0, None, None, None)
+    return int(lib().mas_attention_workspace_bytes(d, 1 if backward else 0))
+
+
+def mas_attention(q, k, v, t_q=None, t_k=None, causal=False, scale=None, cap=0.0, slope=None, doc_start=None,
+                  prefix=None, out=None, lse_out=None, workspace=None, stream=None):
+    """Attention of q [B, Tq, Hq, D] over k, v [B, Tk, Hk, D] (any strides,
+    channels contiguous); returns out [B, Tq, Hq, D].
+
+    scale None: 1 / sqrt(D).  cap > 0: scores become cap * tanh(score / cap).
+    slope [Hq] fp32: minus slope * distance.  t_q, t_k [B] int32: lengths; the
+    queries are the last t_q tokens of the t_k.  causal, doc_start [B, N + 1]
+    and prefix [B, N] int32: see mas.h.  lse_out [B, Hq, Tq] fp32 is what the
+    backward pass takes.  workspace: a uint8 tensor of
+    mas_attention_workspace_bytes, 256-byte aligned, or None."""
+    d = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
+    hq, hk = _heads(q, "q"), _heads(k, "k", q, (d.B, d.Tk, d.Hk, d.D))
+    hv = _heads(v, "v", q, (d.B, d.Tk, d.Hk, d.D))
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    ho = _heads(out, "out", q, q.shape)
+    pl = _arg(lse_out, "lse_out", torch.float32, (d.B, d.Hq, d.Tq), q.device)
+    L = lib()
+    ws, n, keep = _scratch(workspace, L.mas_attention_workspace_bytes(d, 0) if workspace is None else 1, q.device, stream)
+    _check("mas_attention", L.mas_attention(d, hq, hk, hv, ho, pl, ws, n, _stream(stream, q.device)))
+    return out
+
+
+def mas_attention_backward(dout, q, k, v, out, lse, t_q=None, t_k=None, causal=False, scale=None, cap=0.0, slope=None,
+                           doc_start=None, prefix=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dv) of mas_attention from dout [B, Tq, Hq, D], the
+    inputs, and the forward call's out and lse_out; other arguments as there."""
+    d = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
+    kv = (d.B, d.Tk, d.Hk, d.D)
+    hq, hk, hv = _heads(q, "q"), _heads(k, "k", q, kv), _heads(v, "v", q, kv)
+    ho, hg = _heads(out, "out", q, q.shape), _heads(dout, "dout", q, q.shape)
+    if lse is None:
+        raise TypeError("lse must be a device (cuda/hip) tensor")
+    pl = _arg(lse, "lse", torch.float32, (d.B, d.Hq, d.Tq), q.device)
+    dq = _empty(q.shape, q.dtype, q.device, stream) if dq is None else dq
+    dk = _empty(kv, q.dtype, q.device, stream) if dk is None else dk
+    dv = _empty(kv, q.dtype, q.device, stream) if dv is None else dv
+    gq, gk, gv = _heads(dq, "dq", q, q.shape), _heads(dk, "dk", q, kv), _heads(dv, "dv", q, kv)
+    L = lib()
+    ws, n, keep = _scratch(workspace, L.mas_attention_workspace_bytes(d, 1) if workspace is None else 1, q.device, stream)
+    _check("mas_attention_backward",
+           L.mas_attention_backward(d, hg, hq, hk, hv, ho, pl, gq, gk, gv, ws, n, _stream(stream, q.device)))
+    return dq, dk, dv
+
+
+def _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved):
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q must be [B, T, Hq, D] and k [B, T, Hk, D] or None")
+    B, T, Hq, D = q.shape
+    Hk, dev = 0 if k is None else k.shape[2], q.device
+    if (cos is None) != (sin is None) or (cos is not None and cos.dim() != 2):
+        raise ValueError("cos and sin must both be [P, R / 2], or None")
+    P, half = (0, 0) if cos is None else cos.shape
+    return QkDesc(B, T, Hq, Hk, D, 2 * half, P, _DTYPES.get(q.dtype, -1), 1 if interleaved else 0, eps,
+                  _arg(wq, "wq", torch.float32, (D,), dev), _arg(wk, "wk", torch.float32, (D,), dev),
+                  _arg(cos, "cos", torch.float32, (P, half), dev), _arg(sin, "sin", torch.float32, (P, half), dev),
+                  _arg(pos, "pos", torch.int32, (B, T), dev), _arg(t_x, "t_x", torch.int32, (B,), dev))
+
+
+def mas_qk_norm_rope(q, k, wq, wk, cos, sin, pos=None, t_x=None, eps=1e-6, interleaved=False, q_out=None, k_out=None,
+                     stream=None):
+    """Norm of q [B, T, Hq, D] and k [B, T, Hk, D] (k may be None) for each
+    head, weighted by wq, wk [D] fp32 (None: 1), and the rotation of the first
+    R channels by the rows pos [B, T] int32 (None: the token's index) of cos,
+    sin [P, R / 2] fp32; returns (q_out, k_out).  Padding (t >= t_x) becomes
+    zeros.  q_out, k_out may be q, k."""
+    d = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
+    ks = None if k is None else (d.B, d.T, d.Hk, d.D)
+    hq, hk = _heads(q, "q"), None if k is None else _heads(k, "k", q, ks)
+    q_out = _empty(q.shape, q.dtype, q.device, stream) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = _empty(ks, q.dtype, q.device, stream)
+    oq, ok = _heads(q_out, "q_out", q, q.shape), None if k is None else _heads(k_out, "k_out", q, ks)
+    _check("mas_qk_norm_rope", lib().mas_qk_norm_rope(d, hq, hk, oq, ok, _stream(stream, q.device)))
+    return q_out, k_out if k is not None else None
+
+
+def mas_qk_norm_rope_workspace_bytes(q, k) -> int:
+    """Bytes of workspace for mas_qk_norm_rope_backward."""
+    B, T, Hq, D = q.shape
+    return int(lib().mas_qk_norm_rope_workspace_bytes(B, T, Hq, 0 if k is None else k.shape[2], D))
+
+
+def mas_qk_norm_rope_backward(dq_out, dk_out, q, k, wq, wk, cos, sin, pos=None, t_x=None, eps=1e-6, interleaved=False,
+                              dq=None, dk=None, dwq=None, dwk=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dwq, dwk) of mas_qk_norm_rope from those of its
+    outputs and its inputs; dwq, dwk [D] fp32.  dk, dwk are None without k."""
+    d = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
+    dev, ks = q.device, None if k is None else (d.B, d.T, d.Hk, d.D)
+    hq, hk = _heads(q, "q"), None if k is None else _heads(k, "k", q, ks)
+    gq, gk = _heads(dq_out, "dq_out", q, q.shape), None if k is None else _heads(dk_out, "dk_out", q, ks)
+    dq = _empty(q.shape, q.dtype, dev, stream) if dq is None else dq
+    dwq = _empty((d.D,), torch.float32, dev, stream) if dwq is None else dwq
+    if k is not None:
+        dk = _empty(ks, q.dtype, dev, stream) if dk is None else dk
+        dwk = _empty((d.D,), torch.float32, dev, stream) if dwk is None else dwk
+    oq, ok = _heads(dq, "dq", q, q.shape), None if k is None else _heads(dk, "dk", q, ks)
+    pq = _arg(dwq, "dwq", torch.float32, (d.D,), dev)
+    pk = None if k is None else _arg(dwk, "dwk", torch.float32, (d.D,), dev)
+    ws, n, keep = _scratch(workspace, mas_qk_norm_rope_workspace_bytes(q, k) if workspace is None else 1, dev, stream)
+    _check("mas_qk_norm_rope_backward",
+           lib().mas_qk_norm_rope_backward(d, gq, gk, hq, hk, oq, ok, pq, pk, ws, n, _stream(stream, dev)))
+    return (dq, dk, dwq, dwk) if k is not None else (dq, None, dwq, None)
+
+
+def mas_align_loss_workspace_bytes(B: int, T: int, S: int, D: int) -> int:
+    return int(lib().mas_align_loss_workspace_bytes(B, T, S, D))
+
+
+def mas_align_loss(mu, log_sigma, z, row_start, item_weight=None, loss_out=None, dmu=None, dlog_sigma=None, dz=None,
+                   workspace=None, stream=None, gradients=True):
+    """Negative log-likelihood [B] of the frames z [B, S, D] under the rows of
+    mu, log_sigma [B, T, D] (log_sigma None: unit variance) that row_start [B,
+    T + 1] gives them, and the gradients of the items' losses, each times
+    item_weight [B] (None: 1); returns (loss, dmu, dlog_sigma, dz).  dlog_sigma
+    is None without log_sigma unless given; without `gradients` only those given
+    are made."""
+    if mu.dim() != 3 or z.dim() != 3:
+        raise ValueError("mu must be [B, T, D] and z [B, S, D]")
+    B, T, D = mu.shape
+    S, dev = z.shape[1], mu.device
+    f32 = torch.float32
+    pm, pl = _dev_ptr(mu, "mu", f32), _arg(log_sigma, "log_sigma", f32, (B, T, D), dev)
+    pz = _arg(z, "z", f32, (B, S, D), dev)
+    pr = _arg(row_start, "row_start", torch.int32, (B, T + 1), dev)
+    pw = _arg(item_weight, "item_weight", f32, (B,), dev)
+    loss_out = _empty((B,), f32, dev, stream) if loss_out is None else loss_out
+    if gradients:
+        dmu = _empty((B, T, D), f32, dev, stream) if dmu is None else dmu
+        dz = _empty((B, S, D), f32, dev, stream) if dz is None else dz
+        if dlog_sigma is None and log_sigma is not None:
+            dlog_sigma = _empty((B, T, D), f32, dev, stream)
+    po = _arg(loss_out, "loss_out", f32, (B,), dev)
+    gm, gl = _arg(dmu, "dmu", f32, (B, T, D), dev), _arg(dlog_sigma, "dlog_sigma", f32, (B, T, D), dev)
+    gz = _arg(dz, "dz", f32, (B, S, D), dev)
+    L = lib()
+    ws, n, keep = _scratch(workspace, L.mas_align_loss_workspace_bytes(B, T, S, D) if workspace is None else 1, dev, stream)
+    _check("mas_align_loss", L.mas_align_loss(pm, pl, pz, pr, pw, B, T, S, D, po, gm, gl, gz, ws, n, _stream(stream, dev)))
+    return loss_out, dmu, dlog_sigma, dz

@@ -1,0 +1,1100 @@
+// Attention over text tokens and speech frames, forward and backward.
+//
+//   s = scale q.k;  s = cap tanh(s / cap) (with a cap);  s -= slope |place_q - place_k|
+//   p = exp(s - lse) over the keys a query sees, out = sum p v
+//   delta = sum dout out;  dp = dout.v;  ds = p (dp - delta) (1 - tanh^2) scale
+//   dq = sum ds k;  dk = sum ds q;  dv = sum p dout
+//
+// What a query sees is one interval [lo, hi) of keys: its document (or the whole
+// item), cut after its own place where the mask is causal, but never before the
+// end of the document's prefix.  Each lane holds its row's interval in two
+// registers, and a ballot tells whether a block of keys is seen by every row of
+// the wave (no mask), by none (skipped) or by some.
+//
+// The G query heads of a key head form one row axis, row = token * G + head:
+// keys and values are read once for the group, a step of one token still fills
+// a matrix tile with its heads, and dk, dv of shared heads are one sum.
+//
+// Products are 32 x 32 matrix-core tiles, computed transposed: s^T = k q^T, so
+// that a row's scores lie in one lane (and its partner 32 lanes on), and maxima
+// and sums need one exchange.  p^T in that layout is the right-hand operand of
+// out^T = v^T p^T as it stands, if the contraction runs over the keys in the order
+// in which the lanes hold them: lane half h holds keys 8 (r/4) + 4 h + r % 4.
+// v^T is read in that order too, with the transposing LDS reads for 16-bit types.
+// fp32 uses the fp32 matrix cores in the same layout (eight products of depth 2
+// for one of depth 16), so results are at fp32 level in fp32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "mas_attention.h"
+
+namespace mas {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;  // four waves
+constexpr int kWaves = kThreads / 64;
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Eight elements of an operand: one lane's share of 16 steps of a contraction.
+template <class T> struct Frag;
+template <> struct Frag<float> { using type = f32x8; using four = f32x4; };
+template <> struct Frag<_Float16> { using type = half8; using four = half4; };
+template <> struct Frag<__bf16> { using type = bf8; using four = bf4; };
+template <class T> using frag = typename Frag<T>::type;
+template <class T> using four = typename Frag<T>::four;
+
+__device__ __forceinline__ f32x16 mma(half8 a, half8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(bf8 a, bf8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// Row (of the first operand) that register r of an accumulator holds.
+__device__ __forceinline__ int acc_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+// x and its partner's 32 lanes on, in both lanes.
+__device__ __forceinline__ void both_halves(float x, float& lo, float& hi) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  lo = __uint_as_float(r[0]);
+  hi = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float max_halves(float x) {
+  float a, b;
+  both_halves(x, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float add_halves(float x) {
+  float a, b;
+  both_halves(x, a, b);
+  return a + b;
+}
+
+// LDS written by lanes of the wave is read by others of the same wave.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// tanh(x).  exp form: absolute error of about 2^-23; where that is not enough
+// next to x itself (fp32 inputs, |x| < 1/4) the Taylor sum up to x^9, whose next
+// term is below 2^-26 of x there.
+template <class T> __device__ __forceinline__ float tanh_of(float x) {
+  const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2E));
+  const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f);
+  if constexpr (std::is_same<T, float>::value) {
+    const float y = x * x;
+    float s = fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f);
+    s = fmaf(y, s, 2.0f / 15.0f);
+    s = fmaf(y, s, -1.0f / 3.0f);
+    s = fmaf(y * s, x, x);
+    return fabsf(x) < 0.25f ? s : t;
+  }
+  return t;
+}
+
+// 1 / l, and 0 where nothing was summed; NaN stays.
+__device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+struct Interval {
+  int lo, hi;
+};
+
+// Keys that the query at `place` of item b sees; tk is the item's key length.
+__device__ __forceinline__ Interval interval(const AttnParams& p, int b, int place, int tk) {
+  int lo = 0, hi = tk;
+  int pre = 0;
+  if (p.doc_start) {
+    const int32_t* t = p.doc_start + (size_t)b * (p.N + 1);
+    int first = 0, n = p.N + 1;  // starts up to `place`: the first n of them are candidates
+    while (n > 0) {
+      const int step = n / 2;
+      if (t[first + step] <= place) {
+        first += step + 1;
+        n -= step + 1;
+      } else {
+        n = step;
+      }
+    }
+    if (first == 0 || first > p.N) return {0, 0};
+    lo = max(t[first - 1], 0);
+    hi = min(t[first], tk);
+    if (p.prefix) pre = p.prefix[(size_t)b * p.N + first - 1];
+  } else if (p.prefix) {
+    pre = p.prefix[b];
+  }
+  if (p.causal) hi = min(hi, max(place + 1, lo + min(max(pre, 0), tk)));
+  return hi > lo ? Interval{lo, hi} : Interval{0, 0};
+}
+
+__device__ __forceinline__ int clamp_len(const int32_t* t, int b, int n) { return t ? min(max(t[b], 0), n) : n; }
+
+__device__ __forceinline__ int token_of(const AttnParams& p, int row) {
+  return p.g_mul ? (int)__umulhi((uint32_t)row, p.g_mul) : row >> p.g_shift;
+}
+
+// Which (item, key head), tile and part a workgroup works on.  Workgroups go to
+// the eight dies in turn; where there are pairs for all of them, the workgroups of
+// one pair, which read the same keys, are eight apart.
+struct Place {
+  int pair, tile, split;
+  bool idle;
+};
+__device__ __forceinline__ Place place_of(const AttnParams& p) {
+  const uint32_t per = (uint32_t)p.tiles * (uint32_t)p.splits;
+  uint32_t pair = blockIdx.x / per, rest = blockIdx.x % per;
+  if (p.spread) {
+    const uint32_t n = blockIdx.x / 8;
+    pair = n / per * 8 + blockIdx.x % 8;
+    rest = n % per;
+  }
+  return {(int)pair, (int)(rest % (uint32_t)p.tiles), (int)(rest / (uint32_t)p.tiles), pair >= (uint32_t)p.pairs};
+}
+
+template <class T> __device__ __forceinline__ const T* head(const HeadView& v, int b, int h) {
+  return reinterpret_cast<const T*>(v.data) + (int64_t)b * v.sb + (int64_t)h * v.sh;
+}
+template <class T> __device__ __forceinline__ T* head_out(const HeadView& v, int b, int h) {
+  return reinterpret_cast<T*>(v.data) + (int64_t)b * v.sb + (int64_t)h * v.sh;
+}
+
+// n elements from c on of a row of D, zeros past its end.
+template <class T> __device__ __forceinline__ u32x4 load16(const T* row, int c, int D, bool vec) {
+  if (vec) return c < D ? *reinterpret_cast<const u32x4*>(row + c) : u32x4(0);
+  constexpr int E = 16 / sizeof(T);
+  union {
+    T e[E];
+    u32x4 v;
+  } u;
+#pragma unroll
+  for (int i = 0; i < E; ++i) u.e[i] = c + i < D ? row[c + i] : T(0);
+  return u.v;
+}
+
+template <class T> __device__ __forceinline__ frag<T> load_frag(const T* row, int c, int D, bool vec) {
+  union {
+    u32x4 v[sizeof(frag<T>) / 16];
+    frag<T> f;
+  } u;
+  constexpr int E = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(frag<T>) / 16); ++i) u.v[i] = load16(row, c + i * E, D, vec);
+  return u.f;
+}
+
+// A tile of ROWS rows of DP channels on its way from memory to LDS, spread over
+// TEAM threads in 16-byte pieces.
+template <class T, int DP, int ROWS, int TEAM> struct Stage {
+  static constexpr int E = 16 / sizeof(T), CPR = DP / E, N = ROWS * CPR / TEAM;
+  static_assert(ROWS * CPR % TEAM == 0, "whole pieces for every thread");
+  u32x4 r[N];
+  // Rows k0 + i of a head; zeros from `limit` on.
+  __device__ __forceinline__ void load(const T* base, int64_t st, int k0, int limit, int D, bool vec, int tid) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
+      r[n] = u32x4(0);
+      if (k0 + i < limit) r[n] = load16(base + (int64_t)(k0 + i) * st, c, D, vec);
+    }
+  }
+  // Rows of the group's row axis.
+  __device__ __forceinline__ void load_rows(const AttnParams& p, const HeadView& v, int b, int hk, int r0, int limit, int tid) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = r0 + (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
+      r[n] = u32x4(0);
+      if (i < limit) {
+        const int tok = token_of(p, i);
+        r[n] = load16(head<T>(v, b, hk * p.G + (i - tok * p.G)) + (int64_t)tok * v.st, c, p.D, p.vec);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T* lds, int ld, int tid) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
+      *reinterpret_cast<u32x4*>(lds + i * ld + c) = r[n];
+    }
+  }
+};
+
+// Leading dimension of a tile in LDS: 16 bytes more than the row, so that the 32
+// rows of an operand read start on different banks.
+template <class T, int DP> constexpr int kLd = DP + 16 / (int)sizeof(T);
+
+// Operand from rows of a tile: lane l holds row l % 32, channels c + 8 (l / 32) ...
+template <class T> __device__ __forceinline__ frag<T> rows_frag(const T* tile, int ld, int c, int lane) {
+  union {
+    u32x4 v[sizeof(frag<T>) / 16];
+    frag<T> f;
+  } u;
+  const u32x4* at = reinterpret_cast<const u32x4*>(tile + (lane % 32) * ld + c + 8 * (lane / 32));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(frag<T>) / 16); ++i) u.v[i] = at[i];
+  return u.f;
+}
+
+// Operand from columns of a tile: lane l holds channel c + l % 32 of the rows
+// 16 m + 4 (l / 32) + {0..3, 8..11}.
+template <class T> __device__ __forceinline__ frag<T> cols_frag(const T* tile, int ld, int m, int c, int lane) {
+  const int h = lane / 32;
+  if constexpr (sizeof(T) == 4) {
+    frag<T> f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = tile[(16 * m + 8 * (e / 4) + 4 * h + e % 4) * ld + c + lane % 32];
+    return f;
+  } else {
+    // Sixteen lanes read a block of 4 rows and 16 channels, four channels each, and
+    // get it transposed: a channel each, of the four rows.
+    typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+    const int j = lane % 16;
+    const T* at = tile + (16 * m + 4 * h + j / 4) * ld + c + 16 * (lane / 16 % 2) + 4 * (j % 4);
+    union {
+      s16x4 q[2];
+      frag<T> f;
+    } u;
+    u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
+    u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * ld));
+    return u.f;
+  }
+}
+
+// Registers 8 m ... 8 m + 7 of an accumulator as an operand.
+template <class T> __device__ __forceinline__ frag<T> acc_frag(const f32x16& x, int m) {
+  frag<T> f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = (T)x[8 * m + e];
+  return f;
+}
+
+// A row of one head from the transposed accumulators o[DP / 32], times mul: a lane
+// holds four neighbours at a time.  A factor of 0 stands for a row without a
+// result: zeros, whatever the accumulators hold.
+template <class T, int DP> __device__ __forceinline__ void store_row(T* row, const f32x16* o, float mul, int half, int D, bool vec) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int c = 32 * d + acc_row(r, half);
+      four<T> x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (T)(mul != 0.0f ? o[d][r + e] * mul : 0.0f);
+      if (vec) {
+        if (c < D) *reinterpret_cast<four<T>*>(row + c) = x;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < D) row[c + e] = x[e];
+      }
+    }
+}
+
+// A wave's 32 rows: lane l and l + 32 hold row l % 32.
+struct Rows {
+  int row, tok, h;      // of the row axis; its token, its query head
+  int lo, hi, at;       // keys it sees, and its place among the keys
+  bool in, used;        // the row is one of the tensor's; its token is inside the item
+  float slope;          // in powers of two
+};
+__device__ __forceinline__ Rows rows_of(const AttnParams& p, int row, int b, int hk, int tq, int tk) {
+  Rows r;
+  r.row = row;
+  r.in = row < p.rows;
+  r.tok = token_of(p, r.in ? row : 0);
+  r.h = hk * p.G + (r.in ? row - r.tok * p.G : 0);
+  r.used = r.in && r.tok < tq;
+  r.at = r.tok + tk - tq;
+  const Interval s = r.used ? interval(p, b, r.at, tk) : Interval{0, 0};
+  r.lo = s.lo;
+  r.hi = s.hi;
+  r.slope = p.slope ? p.slope[r.h] * kLog2E : 0.0f;
+  return r;
+}
+
+// First and last key that any of the workgroup's rows sees.
+__device__ __forceinline__ Interval key_range(int lo, int hi, int (&lds)[2 * kWaves]) {
+  int a = hi > lo ? lo : 0x7fffffff, z = hi > lo ? hi : 0;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    a = min(a, __shfl_xor(a, s));
+    z = max(z, __shfl_xor(z, s));
+  }
+  if (threadIdx.x % 64 == 0) {
+    lds[threadIdx.x / 64] = a;
+    lds[kWaves + threadIdx.x / 64] = z;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    a = min(a, lds[w]);
+    z = max(z, lds[kWaves + w]);
+  }
+  return a < z ? Interval{a, z} : Interval{0, 0};
+}
+
+enum class Seen { none, some, all };
+// How the wave's rows see the n keys from k on.
+__device__ __forceinline__ Seen seen(int lo, int hi, int k, int n) {
+  if (__ballot(lo < k + n && hi > k) == 0) return Seen::none;
+  return __ballot((lo <= k && hi >= k + n) || hi <= lo) == ~0ull ? Seen::all : Seen::some;
+}
+
+// Scores of a 32 x 32 block, keys from k0 on down the registers, the row's own
+// across: scaled to powers of two, but for a last factor `mul` where nothing but
+// the scale applies.  bend: 1 - tanh^2.
+struct ScoreRule {
+  float scale, cap, mul;  // scale: of the product before the cap, or in powers of two
+  bool capped, sloped;
+};
+__device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
+  ScoreRule s;
+  s.capped = p.cap > 0.0f;
+  s.sloped = p.slope != nullptr;
+  const bool plain = !s.capped && !s.sloped && p.scale > 0.0f;
+  s.scale = s.capped ? p.scale / p.cap : p.scale * kLog2E;
+  s.cap = p.cap * kLog2E;
+  s.mul = plain ? s.scale : 1.0f;
+  return s;
+}
+template <class T, bool BEND> __device__ __forceinline__ void score(f32x16& s, f32x16& bend, const ScoreRule& rule, float slope, int at, int k0, int half) {
+  if (rule.capped) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float t = tanh_of<T>(s[r] * rule.scale);
+      s[r] = t * rule.cap;
+      if (BEND) bend[r] = fmaf(-t, t, 1.0f);
+    }
+  } else if (rule.mul == 1.0f) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= rule.scale;
+  }
+  if (rule.sloped) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf((float)(at - k0 - acc_row(r, half))), s[r]);
+  }
+}
+
+// ------------------------------------------------------------------ forward
+// Keys of a tile: 64, or 32 in fp32, whose rows are twice as long.
+template <class T> constexpr int kTile = sizeof(T) == 4 ? 32 : 64;
+
+// One wave's state: out^T of 32 rows, the running maximum (times mul) and each
+// lane's part of the total.
+template <class T, int DP> struct Forward {
+  frag<T> q[DP / 16];
+  f32x16 o[DP / 32];
+  float m, l;
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = f32x16(0.0f);
+    clear();
+  }
+  // No total: also of a row that sees nothing, which takes part in unmasked blocks.
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY;
+    l = 0.0f;
+  }
+  // NB blocks of 32 keys from k0 on, in LDS.
+  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const ScoreRule& rule, int lane) {
+    const Seen how = seen(w.lo, w.hi, k0, 32 * NB);
+    if (how == Seen::none) return;
+    const int half = lane / 32;
+    f32x16 s[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      s[n] = f32x16(0.0f);
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) s[n] = mma(rows_frag(kt + 32 * n * ld, ld, 16 * c, lane), q[c], s[n]);
+      score<T, false>(s[n], s[n], rule, w.slope, w.at, k0 + 32 * n, half);
+      if (how == Seen::some) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + 32 * n + acc_row(r, half);
+          s[n][r] = key >= w.lo && key < w.hi ? s[n][r] : -INFINITY;
+        }
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+    top = fmaxf(m, max_halves(top) * rule.mul);
+    const float base = top == -INFINITY ? 0.0f : top;
+    if (__ballot(top != m) != 0) {
+      const float shrink = __builtin_amdgcn_exp2f(m - base);
+      l *= shrink;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) o[d] *= shrink;
+      m = top;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], rule.mul, -base));
+        l += s[n][r];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const frag<T> pf = acc_frag<T>(s[n], h);  // p is at most 1; rounded to T for the product, the total is not
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) o[d] = mma(cols_frag(vt, ld, 2 * n + h, 32 * d, lane), pf, o[d]);
+      }
+    }
+  }
+};
+
+template <class T, int DP> __device__ __forceinline__ void load_q(const AttnParams& p, const HeadView& v, const Rows& w, int b, int lane, frag<T> (&q)[DP / 16]) {
+  const T* row = head<T>(v, b, w.h) + (int64_t)w.tok * v.st;
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) q[c] = w.used ? load_frag(row, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+}
+
+// 128 rows a workgroup, 32 a wave; the workgroup shares each tile of keys and
+// values, of which the next is on its way while one is used.
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnParams p) {
+  constexpr int KT = kTile<T>, LD = kLd<T, DP>;
+  __shared__ __align__(16) T kt[2][KT * LD];
+  __shared__ __align__(16) T vt[2][KT * LD];
+  __shared__ int range[2 * kWaves];
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  // The last rows see most where the mask is causal: they start first.
+  const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
+  const Rows w = rows_of(p, 128 * tile + 32 * wave + lane % 32, b, hk, tq, tk);
+  const Interval keys = key_range(w.lo, w.hi, range);
+  const ScoreRule rule = score_rule(p);
+
+  Forward<T, DP> f;
+  load_q<T, DP>(p, p.q, w, b, lane, f.q);
+  f.start();
+
+  const T* kb = head<T>(p.k, b, hk);
+  const T* vb = head<T>(p.v, b, hk);
+  Stage<T, DP, KT, kThreads> ks, vs;
+  const int first = keys.lo / KT * KT;
+  if (first < keys.hi) {
+    ks.load(kb, p.k.st, first, tk, p.D, p.vec, tid);
+    vs.load(vb, p.v.st, first, tk, p.D, p.vec, tid);
+    ks.store(kt[0], LD, tid);
+    vs.store(vt[0], LD, tid);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
+    const bool more = k0 + KT < keys.hi;
+    if (more) {
+      ks.load(kb, p.k.st, k0 + KT, tk, p.D, p.vec, tid);
+      vs.load(vb, p.v.st, k0 + KT, tk, p.D, p.vec, tid);
+    }
+    f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
+    if (more) {
+      ks.store(kt[cur ^ 1], LD, tid);
+      vs.store(vt[cur ^ 1], LD, tid);
+    }
+    __syncthreads();
+  }
+  if (!w.in) return;
+  if (w.hi <= w.lo) f.clear();
+  const float l = add_halves(f.l);
+  store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (f.m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Few rows: 32 a workgroup, whose four waves take the blocks of 32 keys in turn,
+// each with its own maximum, total and sums, joined at the end; with `splits` > 1
+// a workgroup takes a part of the keys and a second kernel joins the parts.
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnParams p) {
+  constexpr int LD = kLd<T, DP>;
+  struct Tiles {
+    T k[32 * LD], v[32 * LD];
+  };
+  struct Join {
+    float o[kWaves - 1][DP / 32 * 16][64], m[kWaves - 1][64], l[kWaves - 1][64];
+  };
+  __shared__ __align__(16) union {
+    Tiles t[kWaves];
+    Join j;
+  } lds;
+  __shared__ int range[2 * kWaves];
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
+  const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
+  Interval keys = key_range(w.lo, w.hi, range);
+  const ScoreRule rule = score_rule(p);
+  keys.lo = max(keys.lo / 32 * 32, at.split * p.span);
+  keys.hi = min(keys.hi, (at.split + 1) * p.span);
+
+  Forward<T, DP> f;
+  load_q<T, DP>(p, p.q, w, b, lane, f.q);
+  f.start();
+
+  const T* kb = head<T>(p.k, b, hk);
+  const T* vb = head<T>(p.v, b, hk);
+  Stage<T, DP, 32, 64> ks, vs;
+  Tiles& mine = lds.t[wave];
+  int k0 = keys.lo + 32 * wave;
+  if (k0 < keys.hi) {
+    ks.load(kb, p.k.st, k0, tk, p.D, p.vec, lane);
+    vs.load(vb, p.v.st, k0, tk, p.D, p.vec, lane);
+  }
+  for (; k0 < keys.hi; k0 += 32 * kWaves) {
+    ks.store(mine.k, LD, lane);
+    vs.store(mine.v, LD, lane);
+    wave_sync();
+    if (k0 + 32 * kWaves < keys.hi) {
+      ks.load(kb, p.k.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+      vs.load(vb, p.v.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+    }
+    f.template step<1>(mine.k, mine.v, LD, k0, w, rule, lane);
+    wave_sync();
+  }
+  if (w.hi <= w.lo) f.clear();
+  __syncthreads();
+  if (wave > 0) {
+    lds.j.m[wave - 1][lane] = f.m;
+    lds.j.l[wave - 1][lane] = f.l;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) lds.j.o[wave - 1][16 * d + r][lane] = f.o[d][r];
+  }
+  __syncthreads();
+  if (wave > 0 || !w.in) return;
+  float top = f.m;
+#pragma unroll
+  for (int i = 0; i < kWaves - 1; ++i) top = fmaxf(top, lds.j.m[i][lane]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float a = __builtin_amdgcn_exp2f(f.m - base), l = f.l * a;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) f.o[d] *= a;
+#pragma unroll
+  for (int i = 0; i < kWaves - 1; ++i) {
+    a = __builtin_amdgcn_exp2f(lds.j.m[i][lane] - base);
+    l = fmaf(a, lds.j.l[i][lane], l);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) f.o[d][r] = fmaf(a, lds.j.o[i][16 * d + r][lane], f.o[d][r]);
+  }
+  l = add_halves(l);
+  if (p.splits > 1) {
+    const size_t slot = ((size_t)at.split * p.pairs + at.pair) * (32 * (size_t)p.tiles) + w.row;
+    float* o = p.part + slot * (p.D + 2);
+    if (lane < 32) {
+      o[p.D] = top;
+      o[p.D + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = 32 * d + acc_row(r, lane / 32);
+        if (c < p.D) o[c] = f.o[d][r];
+      }
+    return;
+  }
+  store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The parts of a row, joined: a wave for each row, two channels a lane.
+template <class T>
+__global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams p) {
+  const size_t n = (size_t)blockIdx.x * kWaves + threadIdx.x / 64;
+  const int lane = threadIdx.x % 64;
+  const int pair = (int)(n / p.rows), row = (int)(n % p.rows);
+  if (pair >= p.pairs) return;
+  const size_t stride = (size_t)p.pairs * 32 * p.tiles * (p.D + 2);
+  const float* o = p.part + ((size_t)pair * 32 * p.tiles + row) * (p.D + 2);
+  float top = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, o[s * stride + p.D]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float l = 0.0f, x[2] = {0.0f, 0.0f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float a = __builtin_amdgcn_exp2f(o[s * stride + p.D] - base);
+    l = fmaf(a, o[s * stride + p.D + 1], l);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (lane + 64 * e < p.D) x[e] = fmaf(a, o[s * stride + lane + 64 * e], x[e]);
+  }
+  const int tok = token_of(p, row), b = pair / p.Hk, h = pair % p.Hk * p.G + row - tok * p.G;
+  T* out = head_out<T>(p.out, b, h) + (int64_t)tok * p.out.st;
+  const float mul = inverse(l);
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (lane + 64 * e < p.D) out[lane + 64 * e] = (T)(mul != 0.0f ? x[e] * mul : 0.0f);
+  if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.Tq + tok] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ----------------------------------------------------------------- backward
+// Sums of the workgroup's four waves, in the first wave: two rounds through LDS.
+template <int N> __device__ __forceinline__ void add_waves(f32x16 (&x)[N], float* lds, int wave, int lane) {
+#pragma unroll
+  for (int from = kWaves / 2; from > 0; from /= 2) {
+    __syncthreads();
+    if (wave >= from && wave < 2 * from) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) lds[((wave - from) * N * 16 + n * 16 + r) * 64 + lane] = x[n][r];
+    }
+    __syncthreads();
+    if (wave < from) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[n][r] += lds[(wave * N * 16 + n * 16 + r) * 64 + lane];
+    }
+  }
+}
+
+// dq of a wave's 32 rows; also delta, which the second kernel needs.
+template <class T, int DP> struct BackwardQ {
+  frag<T> q[DP / 16], g[DP / 16];  // queries and gradients of the output
+  f32x16 dq[DP / 32];
+  float lse, delta;  // lse in powers of two
+  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const ScoreRule& rule, int lane) {
+    const int half = lane / 32;
+#pragma unroll
+    for (int n = 0; n < NB; ++n, kt += 32 * ld, vt += 32 * ld, k0 += 32) {
+      const Seen how = seen(w.lo, w.hi, k0, 32);
+      if (how == Seen::none) continue;
+      f32x16 s(0.0f), dp(0.0f), bend(1.0f);
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) s = mma(rows_frag(kt, ld, 16 * c, lane), q[c], s);
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) dp = mma(rows_frag(vt, ld, 16 * c, lane), g[c], dp);
+      score<T, true>(s, bend, rule, w.slope, w.at, k0, half);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = __builtin_amdgcn_exp2f(fmaf(s[r], rule.mul, -lse)) * (dp[r] - delta);
+        if (rule.capped) x *= bend[r];
+        if (how == Seen::some) {
+          const int key = k0 + acc_row(r, half);
+          x = key >= w.lo && key < w.hi ? x : 0.0f;
+        }
+        s[r] = x;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const frag<T> sf = acc_frag<T>(s, h);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) dq[d] = mma(cols_frag(kt, ld, h, 32 * d, lane), sf, dq[d]);
+      }
+    }
+  }
+};
+
+// FEW: 32 rows a workgroup, its waves take the blocks of keys in turn; else 128
+// rows a workgroup with shared tiles, as in the forward pass.
+template <class T, int DP, bool FEW>
+__global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_attention_dq(const AttnParams p) {
+  constexpr int KT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
+  __shared__ __align__(16) T kt[SETS][KT * LD];
+  __shared__ __align__(16) T vt[SETS][KT * LD];
+  __shared__ int range[2 * kWaves];
+  static_assert(!FEW || sizeof(kt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
+  const Rows w = rows_of(p, FEW ? 32 * tile + lane % 32 : 128 * tile + 32 * wave + lane % 32, b, hk, tq, tk);
+  const Interval keys = key_range(w.lo, w.hi, range);
+  const ScoreRule rule = score_rule(p);
+
+  BackwardQ<T, DP> f;
+  load_q<T, DP>(p, p.q, w, b, lane, f.q);
+  load_q<T, DP>(p, p.dout, w, b, lane, f.g);
+  f.delta = 0.0f;
+  {
+    const T* row = head<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+      const frag<T> o = w.used ? load_frag(row, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f.delta = fmaf((float)o[e], (float)f.g[c][e], f.delta);
+    }
+    f.delta = add_halves(f.delta);
+  }
+  f.lse = w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f;
+  if (w.in && lane < 32 && (!FEW || wave == 0)) {
+    p.stat[(size_t)at.pair * p.rows + w.row] = float2{f.lse, f.delta};
+    if (hk == 0 && w.row == w.tok * p.G) p.see[(size_t)b * p.Tq + w.tok] = int2{w.lo, w.hi};
+  }
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) f.dq[d] = f32x16(0.0f);
+
+  const T* kb = head<T>(p.k, b, hk);
+  const T* vb = head<T>(p.v, b, hk);
+  const int first = keys.lo / KT * KT;
+  if constexpr (FEW) {
+    Stage<T, DP, 32, 64> ks, vs;
+    int k0 = first + 32 * wave;
+    if (k0 < keys.hi) {
+      ks.load(kb, p.k.st, k0, tk, p.D, p.vec, lane);
+      vs.load(vb, p.v.st, k0, tk, p.D, p.vec, lane);
+    }
+    for (; k0 < keys.hi; k0 += 32 * kWaves) {
+      ks.store(kt[wave], LD, lane);
+      vs.store(vt[wave], LD, lane);
+      wave_sync();
+      if (k0 + 32 * kWaves < keys.hi) {
+        ks.load(kb, p.k.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+        vs.load(vb, p.v.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+      }
+      f.template step<1>(kt[wave], vt[wave], LD, k0, w, rule, lane);
+      wave_sync();
+    }
+    add_waves(f.dq, reinterpret_cast<float*>(kt), wave, lane);
+    if (wave > 0) return;
+  } else {
+    Stage<T, DP, KT, kThreads> ks, vs;
+    if (first < keys.hi) {
+      ks.load(kb, p.k.st, first, tk, p.D, p.vec, tid);
+      vs.load(vb, p.v.st, first, tk, p.D, p.vec, tid);
+      ks.store(kt[0], LD, tid);
+      vs.store(vt[0], LD, tid);
+    }
+    __syncthreads();
+    int cur = 0;
+    for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
+      const bool more = k0 + KT < keys.hi;
+      if (more) {
+        ks.load(kb, p.k.st, k0 + KT, tk, p.D, p.vec, tid);
+        vs.load(vb, p.v.st, k0 + KT, tk, p.D, p.vec, tid);
+      }
+      f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
+      if (more) {
+        ks.store(kt[cur ^ 1], LD, tid);
+        vs.store(vt[cur ^ 1], LD, tid);
+      }
+      __syncthreads();
+    }
+  }
+  if (w.in) store_row<T, DP>(head_out<T>(p.dq, b, w.h) + (int64_t)w.tok * p.dq.st, f.dq, w.hi > w.lo ? p.scale : 0.0f, lane / 32, p.D, p.vec);
+}
+
+// What the rows of a tile bring along: the statistics and the keys they see.
+struct RowInfo {
+  float lse, delta, slope;
+  int lo, hi, at;
+};
+template <int ROWS> struct RowTable {
+  float lse[ROWS], delta[ROWS], slope[ROWS];
+  int lo[ROWS], hi[ROWS], at[ROWS];
+  __device__ __forceinline__ void put(int i, const RowInfo& x) {
+    lse[i] = x.lse;
+    delta[i] = x.delta;
+    slope[i] = x.slope;
+    lo[i] = x.lo;
+    hi[i] = x.hi;
+    at[i] = x.at;
+  }
+};
+__device__ __forceinline__ RowInfo row_info(const AttnParams& p, int b, int hk, int row, int limit, int shift) {
+  RowInfo x = {0.0f, 0.0f, 0.0f, 0, 0, 0};
+  if (row < limit) {
+    const int tok = token_of(p, row);
+    const float2 s = p.stat[((size_t)b * p.Hk + hk) * p.rows + row];
+    const int2 see = p.see[(size_t)b * p.Tq + tok];
+    x.lse = s.x;
+    x.delta = s.y;
+    x.lo = see.x;
+    x.hi = see.y;
+    x.at = tok + shift;
+    x.slope = p.slope ? p.slope[hk * p.G + row - tok * p.G] * kLog2E : 0.0f;
+  }
+  return x;
+}
+
+// dk, dv of a wave's 32 keys (lane l and l + 32 hold key l % 32): s = q k^T with
+// the rows down the registers, so that p and ds are operands of dv^T = dout^T p
+// and dk^T = q^T ds as they stand.
+template <class T, int DP> struct BackwardK {
+  frag<T> k[DP / 16], v[DP / 16];
+  f32x16 dk[DP / 32], dv[DP / 32];
+  // 32 rows in LDS against the keys from k0 on.
+  template <int ROWS> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int k0, const ScoreRule& rule, int lane) {
+    const int half = lane / 32, key = k0 + lane % 32;
+    const Seen how = seen(t.lo[i0 + lane % 32], t.hi[i0 + lane % 32], k0, 32);
+    if (how == Seen::none) return;
+    // Rows that see nothing have no statistics: they are masked, not taken for full.
+    const bool mask = __ballot(t.lo[i0 + lane % 32] <= k0 && t.hi[i0 + lane % 32] >= k0 + 32) != ~0ull;
+    f32x16 s(0.0f), dp(0.0f);
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) s = mma(rows_frag(qt, ld, 16 * c, lane), k[c], s);
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) dp = mma(rows_frag(gt, ld, 16 * c, lane), v[c], dp);
+#pragma unroll
+    for (int r4 = 0; r4 < 16; r4 += 4) {
+      const int i = i0 + acc_row(r4, half);
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(&t.lse[i]), delta = *reinterpret_cast<const f32x4*>(&t.delta[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = r4 + e;
+        float x = s[r], bend = 1.0f;
+        if (rule.capped) {
+          const float y = tanh_of<T>(x * rule.scale);
+          x = y * rule.cap;
+          bend = fmaf(-y, y, 1.0f);
+        } else if (rule.mul == 1.0f) {
+          x *= rule.scale;
+        }
+        if (rule.sloped) x = fmaf(-t.slope[i + e], fabsf((float)(t.at[i + e] - key)), x);
+        float pr = __builtin_amdgcn_exp2f(fmaf(x, rule.mul, -lse[e]));
+        float ds = pr * (dp[r] - delta[e]) * bend;
+        if (mask) {
+          const bool sees = key >= t.lo[i + e] && key < t.hi[i + e];
+          pr = sees ? pr : 0.0f;
+          ds = sees ? ds : 0.0f;
+        }
+        s[r] = pr;
+        dp[r] = ds;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const frag<T> pf = acc_frag<T>(s, h), sf = acc_frag<T>(dp, h);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        dv[d] = mma(cols_frag(gt, ld, h, 32 * d, lane), pf, dv[d]);
+        dk[d] = mma(cols_frag(qt, ld, h, 32 * d, lane), sf, dk[d]);
+      }
+    }
+  }
+};
+
+// FEW: 32 keys a workgroup, its waves take the blocks of 32 rows in turn; else
+// 128 keys a workgroup, 32 a wave, with shared tiles of rows.
+template <class T, int DP, bool FEW>
+__global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
+  constexpr int RT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
+  __shared__ __align__(16) T qt[SETS][RT * LD];
+  __shared__ __align__(16) T gt[SETS][RT * LD];
+  __shared__ __align__(16) RowTable<RT> table[SETS];
+  __shared__ int range[2 * kWaves];
+  static_assert(!FEW || sizeof(qt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  constexpr int KEYS = FEW ? 32 : 128;
+  const int kb0 = KEYS * at.tile, k0 = FEW ? kb0 : kb0 + 32 * wave;
+  const int key = k0 + lane % 32;
+  const bool in = key < p.Tk;
+  // The rows that see any of the workgroup's keys.
+  int lo = 0x7fffffff, hi = 0;
+  if (kb0 < tk) {
+    for (int t = tid; t < tq; t += kThreads) {
+      const int2 s = p.see[(size_t)b * p.Tq + t];
+      if (s.x < kb0 + KEYS && s.y > kb0) {
+        lo = min(lo, t);
+        hi = t + 1;
+      }
+    }
+  }
+  Interval rows = key_range(lo, hi, range);
+  rows.lo *= p.G;
+  rows.hi *= p.G;
+  const ScoreRule rule = score_rule(p);
+
+  BackwardK<T, DP> f;
+  {
+    const T* kr = head<T>(p.k, b, hk) + (int64_t)key * p.k.st;
+    const T* vr = head<T>(p.v, b, hk) + (int64_t)key * p.v.st;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+      f.k[c] = key < tk ? load_frag(kr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+      f.v[c] = key < tk ? load_frag(vr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) f.dk[d] = f.dv[d] = f32x16(0.0f);
+
+  const int first = rows.lo / RT * RT, shift = tk - tq;
+  if constexpr (FEW) {
+    Stage<T, DP, 32, 64> qs, gs;
+    RowInfo info;
+    int r0 = first + 32 * wave;
+    const auto fetch = [&](int r) {
+      qs.load_rows(p, p.q, b, hk, r, rows.hi, lane);
+      gs.load_rows(p, p.dout, b, hk, r, rows.hi, lane);
+      if (lane < 32) info = row_info(p, b, hk, r + lane, rows.hi, shift);
+    };
+    if (r0 < rows.hi) fetch(r0);
+    for (; r0 < rows.hi; r0 += 32 * kWaves) {
+      qs.store(qt[wave], LD, lane);
+      gs.store(gt[wave], LD, lane);
+      if (lane < 32) table[wave].put(lane, info);
+      wave_sync();
+      if (r0 + 32 * kWaves < rows.hi) fetch(r0 + 32 * kWaves);
+      f.step(qt[wave], gt[wave], LD, table[wave], 0, k0, rule, lane);
+      wave_sync();
+    }
+    add_waves(f.dk, reinterpret_cast<float*>(qt), wave, lane);
+    add_waves(f.dv, reinterpret_cast<float*>(qt), wave, lane);
+    if (wave > 0) return;
+  } else {
+    Stage<T, DP, RT, kThreads> qs, gs;
+    RowInfo info;
+    const auto fetch = [&](int r) {
+      qs.load_rows(p, p.q, b, hk, r, rows.hi, tid);
+      gs.load_rows(p, p.dout, b, hk, r, rows.hi, tid);
+      if (tid < RT) info = row_info(p, b, hk, r + tid, rows.hi, shift);
+    };
+    const auto put = [&](int to) {
+      qs.store(qt[to], LD, tid);
+      gs.store(gt[to], LD, tid);
+      if (tid < RT) table[to].put(tid, info);
+    };
+    if (first < rows.hi) {
+      fetch(first);
+      put(0);
+    }
+    __syncthreads();
+    int cur = 0;
+    for (int r0 = first; r0 < rows.hi; r0 += RT, cur ^= 1) {
+      const bool more = r0 + RT < rows.hi;
+      if (more) fetch(r0 + RT);
+#pragma unroll
+      for (int n = 0; n < RT / 32; ++n) f.step(qt[cur] + 32 * n * LD, gt[cur] + 32 * n * LD, LD, table[cur], 32 * n, k0, rule, lane);
+      if (more) put(cur ^ 1);
+      __syncthreads();
+    }
+  }
+  if (!in) return;
+  store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, f.dk, p.scale, lane / 32, p.D, p.vec);
+  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, f.dv, 1.0f, lane / 32, p.D, p.vec);
+}
+
+// Workgroups, and how place_of deals them out: over the dies if the last, partly
+// used round of eight pairs is a small part.
+uint32_t grid_of(AttnParams& p) {
+  p.spread = p.pairs % 8 == 0 || p.pairs >= 64;
+  return (uint32_t)(p.spread ? (p.pairs + 7) / 8 * 8 : p.pairs) * (uint32_t)p.tiles * (uint32_t)p.splits;
+}
+
+template <class T, int DP> hipError_t forward(AttnParams p, const AttnPlan& plan, hipStream_t stream) {
+  const uint32_t grid = grid_of(p);
+  if (!plan.small) {
+    hipLaunchKernelGGL((mas_attention_rows<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((mas_attention_keys<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const uint64_t rows = (uint64_t)p.pairs * p.rows;
+  hipLaunchKernelGGL((mas_attention_join<T>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream) {
+  p.splits = 1;
+  // 128 rows a workgroup where those fill the 256 compute units, else 32.
+  p.tiles = (p.rows + 127) / 128;
+  const bool few_rows = (int64_t)p.tiles * p.pairs < 256;
+  if (few_rows) p.tiles = (p.rows + 31) / 32;
+  uint32_t grid = grid_of(p);
+  if (few_rows)
+    hipLaunchKernelGGL((mas_attention_dq<T, DP, true>), dim3(grid), dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((mas_attention_dq<T, DP, false>), dim3(grid), dim3(kThreads), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  p.tiles = (p.Tk + 127) / 128;
+  const bool few_keys = (int64_t)p.tiles * p.pairs < 256;
+  if (few_keys) p.tiles = (p.Tk + 31) / 32;
+  grid = grid_of(p);
+  if (few_keys)
+    hipLaunchKernelGGL((mas_attention_dkv<T, DP, true>), dim3(grid), dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((mas_attention_dkv<T, DP, false>), dim3(grid), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <class T, class F> hipError_t by_width(int D, F&& f) {
+  if (D <= 32) return f(std::integral_constant<int, 32>());
+  if (D <= 64) return f(std::integral_constant<int, 64>());
+  if (D <= 96) return f(std::integral_constant<int, 96>());
+  return f(std::integral_constant<int, 128>());
+}
+
+}  // namespace
+
+AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk) {
+  AttnPlan a;
+  a.splits = 1;
+  a.span = Tk;
+  a.tiles = (rows + 127) / 128;
+  a.small = (int64_t)a.tiles * pairs < 256;
+  if (!a.small) return a;
+  a.tiles = (rows + 31) / 32;
+  // Parts of at least 128 keys, a block for every wave, until two workgroups a
+  // compute unit are there.
+  const int64_t groups = (int64_t)a.tiles * pairs;
+  int64_t want = (512 + groups - 1) / groups;
+  const int64_t most = (Tk + 127) / 128;
+  if (want > most) want = most;
+  a.span = (int32_t)(((Tk + want - 1) / want + 127) / 128 * 128);
+  a.splits = (Tk + a.span - 1) / a.span;
+  return a;
+}
+
+size_t attention_part_bytes(const AttnPlan& a, int32_t pairs, int32_t D) {
+  return a.splits > 1 ? (size_t)a.splits * pairs * 32 * a.tiles * (D + 2) * sizeof(float) : 0;
+}
+
+hipError_t launch_attention(AttnParams p, int dtype, const AttnPlan& plan, hipStream_t stream) {
+  p.tiles = plan.tiles;
+  p.splits = plan.splits;
+  p.span = plan.span;
+  const auto go = [&](auto t) {
+    using T = decltype(t);
+    return by_width<T>(p.D, [&](auto dp) { return forward<T, decltype(dp)::value>(p, plan, stream); });
+  };
+  if (dtype == kF32) return go(0.0f);
+  if (dtype == kF16) return go((_Float16)0.0f);
+  return go((__bf16)0.0f);
+}
+
+hipError_t launch_attention_backward(AttnParams p, int dtype, hipStream_t stream) {
+  const auto go = [&](auto t) {
+    using T = decltype(t);
+    return by_width<T>(p.D, [&](auto dp) { return backward<T, decltype(dp)::value>(p, stream); });
+  };
+  if (dtype == kF32) return go(0.0f);
+  if (dtype == kF16) return go((_Float16)0.0f);
+  return go((__bf16)0.0f);
+}
+
+}  // namespace mas
