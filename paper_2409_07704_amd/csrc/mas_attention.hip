@@ -46,8 +46,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;  // four waves
 constexpr int kWaves = kThreads / 64;
+constexpr int kMaxWaves = 8;
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.0f;  // powers of two
 
 // Eight elements of an operand: one lane's share of 16 steps of a contraction.
 template <class T> struct Frag;
@@ -199,44 +201,81 @@ template <class T> __device__ __forceinline__ frag<T> load_frag(const T* row, in
 }
 
 // A tile of ROWS rows of DP channels on its way from memory to LDS, spread over
-// TEAM threads in 16-byte pieces.
+// TEAM threads in 16-byte pieces.  Where the tile is inside the tensor, its rows are
+// whole pieces and its extent fits 32 bits, a piece's place in the tile is found
+// once and a tile costs one load each.
 template <class T, int DP, int ROWS, int TEAM> struct Stage {
   static constexpr int E = 16 / sizeof(T), CPR = DP / E, N = ROWS * CPR / TEAM;
   static_assert(ROWS * CPR % TEAM == 0, "whole pieces for every thread");
   u32x4 r[N];
-  // Rows k0 + i of a head; zeros from `limit` on.
-  __device__ __forceinline__ void load(const T* base, int64_t st, int k0, int limit, int D, bool vec, int tid) {
+  uint32_t off[N];
+  bool fast;
+  static __device__ __forceinline__ int row(int n, int tid) { return (tid + n * TEAM) / CPR; }
+  static __device__ __forceinline__ int col(int n, int tid) { return (tid + n * TEAM) % CPR * E; }
+  // Rows of one head, st apart.
+  __device__ __forceinline__ void init(const AttnParams& p, int64_t st, int tid) {
+    fast = p.vec && st < (1 << 30) / (ROWS * (int)sizeof(T));
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int i = (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
       r[n] = u32x4(0);
-      if (k0 + i < limit) r[n] = load16(base + (int64_t)(k0 + i) * st, c, D, vec);
+      off[n] = (uint32_t)(row(n, tid) * (int)st + col(n, tid)) * (uint32_t)sizeof(T);
     }
   }
-  // Rows of the group's row axis.
-  __device__ __forceinline__ void load_rows(const AttnParams& p, const HeadView& v, int b, int hk, int r0, int limit, int tid) {
+  // Rows of the group's row axis, tiles of which start with a token.
+  __device__ __forceinline__ void init_rows(const AttnParams& p, const HeadView& v, int tid) {
+    fast = p.vec && 32 % p.G == 0 && v.st < (1 << 29) / (ROWS * (int)sizeof(T)) && v.sh < (1 << 29) / (ROWS * (int)sizeof(T));
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int i = r0 + (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
       r[n] = u32x4(0);
+      const int i = row(n, tid);
+      off[n] = (uint32_t)((i >> p.g_shift) * (int)v.st + (i & (p.G - 1)) * (int)v.sh + col(n, tid)) * (uint32_t)sizeof(T);
+    }
+  }
+  __device__ __forceinline__ void load_whole(const void* tile, int D, int tid) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (col(n, tid) < D) r[n] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(tile) + off[n]);
+  }
+  // Rows k0 + i of a head; zeros from `limit` on.
+  __device__ __forceinline__ void load(const AttnParams& p, const T* base, int64_t st, int k0, int limit, int tid) {
+    if (fast && k0 + ROWS <= limit) return load_whole(base + k0 * st, p.D, tid);
+#pragma unroll 1
+    for (int n = 0; n < N; ++n) {
+      const int i = k0 + row(n, tid);
+      const u32x4 x = i < limit ? load16(base + (int64_t)i * st, col(n, tid), p.D, p.vec) : u32x4(0);
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+        if (m == n) r[m] = x;
+    }
+  }
+  // Rows r0 + i of the group's row axis, r0 a multiple of 32.
+  __device__ __forceinline__ void load_rows(const AttnParams& p, const HeadView& v, int b, int hk, int r0, int limit, int tid) {
+    if (fast && r0 + ROWS <= limit) return load_whole(head<T>(v, b, hk * p.G) + (int64_t)(r0 >> p.g_shift) * v.st, p.D, tid);
+#pragma unroll 1
+    for (int n = 0; n < N; ++n) {
+      const int i = r0 + row(n, tid);
+      u32x4 x(0);
       if (i < limit) {
         const int tok = token_of(p, i);
-        r[n] = load16(head<T>(v, b, hk * p.G + (i - tok * p.G)) + (int64_t)tok * v.st, c, p.D, p.vec);
+        x = load16(head<T>(v, b, hk * p.G + (i - tok * p.G)) + (int64_t)tok * v.st, col(n, tid), p.D, p.vec);
       }
+#pragma unroll
+      for (int m = 0; m < N; ++m)
+        if (m == n) r[m] = x;
     }
   }
   __device__ __forceinline__ void store(T* lds, int ld, int tid) const {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const int i = (tid + n * TEAM) / CPR, c = (tid + n * TEAM) % CPR * E;
-      *reinterpret_cast<u32x4*>(lds + i * ld + c) = r[n];
-    }
+    for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n, tid) * ld + col(n, tid)) = r[n];
   }
 };
 
 // Leading dimension of a tile in LDS: 16 bytes more than the row, so that the 32
 // rows of an operand read start on different banks.
 template <class T, int DP> constexpr int kLd = DP + 16 / (int)sizeof(T);
+// And of a tile whose columns are read: the four rows of a transposing read on
+// different banks.
+template <class T, int DP> constexpr int kLdCols = sizeof(T) == 4 ? DP : DP % 64 == 0 ? DP + 16 : DP + 48;
 
 // Operand from rows of a tile: lane l holds row l % 32, channels c + 8 (l / 32) ...
 template <class T> __device__ __forceinline__ frag<T> rows_frag(const T* tile, int ld, int c, int lane) {
@@ -327,8 +366,8 @@ __device__ __forceinline__ Rows rows_of(const AttnParams& p, int row, int b, int
   return r;
 }
 
-// First and last key that any of the workgroup's rows sees.
-__device__ __forceinline__ Interval key_range(int lo, int hi, int (&lds)[2 * kWaves]) {
+// First and last number of the intervals that the workgroup's threads hold.
+__device__ __forceinline__ Interval key_range(int lo, int hi, int (&lds)[2 * kMaxWaves]) {
   int a = hi > lo ? lo : 0x7fffffff, z = hi > lo ? hi : 0;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
@@ -337,14 +376,15 @@ __device__ __forceinline__ Interval key_range(int lo, int hi, int (&lds)[2 * kWa
   }
   if (threadIdx.x % 64 == 0) {
     lds[threadIdx.x / 64] = a;
-    lds[kWaves + threadIdx.x / 64] = z;
+    lds[kMaxWaves + threadIdx.x / 64] = z;
   }
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) {
     a = min(a, lds[w]);
-    z = max(z, lds[kWaves + w]);
+    z = max(z, lds[kMaxWaves + w]);
   }
+  a = __builtin_amdgcn_readfirstlane(a);
+  z = __builtin_amdgcn_readfirstlane(z);
   return a < z ? Interval{a, z} : Interval{0, 0};
 }
 
@@ -355,47 +395,27 @@ __device__ __forceinline__ Seen seen(int lo, int hi, int k, int n) {
   return __ballot((lo <= k && hi >= k + n) || hi <= lo) == ~0ull ? Seen::all : Seen::some;
 }
 
-// Scores of a 32 x 32 block, keys from k0 on down the registers, the row's own
-// across: scaled to powers of two, but for a last factor `mul` where nothing but
-// the scale applies.  bend: 1 - tanh^2.
+// From products to scores, in powers of two: x mul - slope distance, with x the
+// product, or tanh(product pre) with a cap.
 struct ScoreRule {
-  float scale, cap, mul;  // scale: of the product before the cap, or in powers of two
+  float pre, mul;
   bool capped, sloped;
 };
 __device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
   ScoreRule s;
   s.capped = p.cap > 0.0f;
   s.sloped = p.slope != nullptr;
-  const bool plain = !s.capped && !s.sloped && p.scale > 0.0f;
-  s.scale = s.capped ? p.scale / p.cap : p.scale * kLog2E;
-  s.cap = p.cap * kLog2E;
-  s.mul = plain ? s.scale : 1.0f;
+  s.pre = s.capped ? p.scale / p.cap : 1.0f;
+  s.mul = (s.capped ? p.cap : p.scale) * kLog2E;
   return s;
-}
-template <class T, bool BEND> __device__ __forceinline__ void score(f32x16& s, f32x16& bend, const ScoreRule& rule, float slope, int at, int k0, int half) {
-  if (rule.capped) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float t = tanh_of<T>(s[r] * rule.scale);
-      s[r] = t * rule.cap;
-      if (BEND) bend[r] = fmaf(-t, t, 1.0f);
-    }
-  } else if (rule.mul == 1.0f) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] *= rule.scale;
-  }
-  if (rule.sloped) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = fmaf(-slope, fabsf((float)(at - k0 - acc_row(r, half))), s[r]);
-  }
 }
 
 // ------------------------------------------------------------------ forward
 // Keys of a tile: 64, or 32 in fp32, whose rows are twice as long.
 template <class T> constexpr int kTile = sizeof(T) == 4 ? 32 : 64;
 
-// One wave's state: out^T of 32 rows, the running maximum (times mul) and each
-// lane's part of the total.
+// One wave's state: out^T of 32 rows, the reference of the exponents (a running
+// maximum, at most kSlack behind) and each lane's part of the total.
 template <class T, int DP> struct Forward {
   frag<T> q[DP / 16];
   f32x16 o[DP / 32];
@@ -411,51 +431,74 @@ template <class T, int DP> struct Forward {
     l = 0.0f;
   }
   // NB blocks of 32 keys from k0 on, in LDS.
-  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const ScoreRule& rule, int lane) {
+  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int ldv, int k0, const Rows& w, const ScoreRule& rule, int lane) {
     const Seen how = seen(w.lo, w.hi, k0, 32 * NB);
     if (how == Seen::none) return;
     const int half = lane / 32;
+    // Scores stay short of their last factor, which the exponent's argument brings in,
+    // unless a distance comes between or the factor turns their order round.
+    const bool general = rule.sloped || rule.mul < 0.0f;
+    const float mul = general ? 1.0f : rule.mul;
     f32x16 s[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       s[n] = f32x16(0.0f);
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) s[n] = mma(rows_frag(kt + 32 * n * ld, ld, 16 * c, lane), q[c], s[n]);
-      score<T, false>(s[n], s[n], rule, w.slope, w.at, k0 + 32 * n, half);
-      if (how == Seen::some) {
+    }
+    if (rule.capped) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] = tanh_of<T>(s[n][r] * rule.pre);
+    }
+    if (general) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const float d = (float)(w.at - k0 - 32 * n - 4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] = fmaf(-w.slope, fabsf(d - acc_row(r, 0)), s[n][r] * rule.mul);
+      }
+    }
+    if (how == Seen::some) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + 32 * n + acc_row(r, half);
           s[n][r] = key >= w.lo && key < w.hi ? s[n][r] : -INFINITY;
         }
-      }
     }
     float top = s[0][0];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
-    top = fmaxf(m, max_halves(top) * rule.mul);
-    const float base = top == -INFINITY ? 0.0f : top;
-    if (__ballot(top != m) != 0) {
-      const float shrink = __builtin_amdgcn_exp2f(m - base);
+    top = max_halves(top) * mul;
+    // The reference of the exponents moves only when a score passes it by more than
+    // kSlack: p is at most 2^kSlack then, which all types hold, and the sums are
+    // seldom rescaled.
+    if (__ballot(top > m + kSlack) != 0) {
+      const float to = fmaxf(m, top);
+      const float shrink = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
       l *= shrink;
 #pragma unroll
       for (int d = 0; d < DP / 32; ++d) o[d] *= shrink;
-      m = top;
+      m = to;
     }
+    const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], rule.mul, -base));
+        s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], mul, -base));
         l += s[n][r];
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const frag<T> pf = acc_frag<T>(s[n], h);  // p is at most 1; rounded to T for the product, the total is not
+        const frag<T> pf = acc_frag<T>(s[n], h);  // rounded to T for the product; the total is not
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) o[d] = mma(cols_frag(vt, ld, 2 * n + h, 32 * d, lane), pf, o[d]);
+        for (int d = 0; d < DP / 32; ++d) o[d] = mma(cols_frag(vt, ldv, 2 * n + h, 32 * d, lane), pf, o[d]);
       }
     }
   }
@@ -471,10 +514,10 @@ template <class T, int DP> __device__ __forceinline__ void load_q(const AttnPara
 // values, of which the next is on its way while one is used.
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnParams p) {
-  constexpr int KT = kTile<T>, LD = kLd<T, DP>;
+  constexpr int KT = kTile<T>, LD = kLd<T, DP>, LDV = kLdCols<T, DP>;
   __shared__ __align__(16) T kt[2][KT * LD];
-  __shared__ __align__(16) T vt[2][KT * LD];
-  __shared__ int range[2 * kWaves];
+  __shared__ __align__(16) T vt[2][KT * LDV];
+  __shared__ int range[2 * kMaxWaves];
   const Place at = place_of(p);
   if (at.idle) return;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
@@ -493,25 +536,27 @@ __global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnPara
   const T* kb = head<T>(p.k, b, hk);
   const T* vb = head<T>(p.v, b, hk);
   Stage<T, DP, KT, kThreads> ks, vs;
+  ks.init(p, p.k.st, tid);
+  vs.init(p, p.v.st, tid);
   const int first = keys.lo / KT * KT;
   if (first < keys.hi) {
-    ks.load(kb, p.k.st, first, tk, p.D, p.vec, tid);
-    vs.load(vb, p.v.st, first, tk, p.D, p.vec, tid);
+    ks.load(p, kb, p.k.st, first, tk, tid);
+    vs.load(p, vb, p.v.st, first, tk, tid);
     ks.store(kt[0], LD, tid);
-    vs.store(vt[0], LD, tid);
+    vs.store(vt[0], LDV, tid);
   }
   __syncthreads();
   int cur = 0;
   for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
     const bool more = k0 + KT < keys.hi;
     if (more) {
-      ks.load(kb, p.k.st, k0 + KT, tk, p.D, p.vec, tid);
-      vs.load(vb, p.v.st, k0 + KT, tk, p.D, p.vec, tid);
+      ks.load(p, kb, p.k.st, k0 + KT, tk, tid);
+      vs.load(p, vb, p.v.st, k0 + KT, tk, tid);
     }
-    f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
+    f.template step<KT / 32>(kt[cur], vt[cur], LD, LDV, k0, w, rule, lane);
     if (more) {
       ks.store(kt[cur ^ 1], LD, tid);
-      vs.store(vt[cur ^ 1], LD, tid);
+      vs.store(vt[cur ^ 1], LDV, tid);
     }
     __syncthreads();
   }
@@ -527,9 +572,9 @@ __global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnPara
 // a workgroup takes a part of the keys and a second kernel joins the parts.
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnParams p) {
-  constexpr int LD = kLd<T, DP>;
+  constexpr int LD = kLd<T, DP>, LDV = kLdCols<T, DP>;
   struct Tiles {
-    T k[32 * LD], v[32 * LD];
+    T k[32 * LD], v[32 * LDV];
   };
   struct Join {
     float o[kWaves - 1][DP / 32 * 16][64], m[kWaves - 1][64], l[kWaves - 1][64];
@@ -538,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
     Tiles t[kWaves];
     Join j;
   } lds;
-  __shared__ int range[2 * kWaves];
+  __shared__ int range[2 * kMaxWaves];
   const Place at = place_of(p);
   if (at.idle) return;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
@@ -558,21 +603,23 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   const T* kb = head<T>(p.k, b, hk);
   const T* vb = head<T>(p.v, b, hk);
   Stage<T, DP, 32, 64> ks, vs;
+  ks.init(p, p.k.st, lane);
+  vs.init(p, p.v.st, lane);
   Tiles& mine = lds.t[wave];
   int k0 = keys.lo + 32 * wave;
   if (k0 < keys.hi) {
-    ks.load(kb, p.k.st, k0, tk, p.D, p.vec, lane);
-    vs.load(vb, p.v.st, k0, tk, p.D, p.vec, lane);
+    ks.load(p, kb, p.k.st, k0, tk, lane);
+    vs.load(p, vb, p.v.st, k0, tk, lane);
   }
   for (; k0 < keys.hi; k0 += 32 * kWaves) {
     ks.store(mine.k, LD, lane);
-    vs.store(mine.v, LD, lane);
+    vs.store(mine.v, LDV, lane);
     wave_sync();
     if (k0 + 32 * kWaves < keys.hi) {
-      ks.load(kb, p.k.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
-      vs.load(vb, p.v.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+      ks.load(p, kb, p.k.st, k0 + 32 * kWaves, tk, lane);
+      vs.load(p, vb, p.v.st, k0 + 32 * kWaves, tk, lane);
     }
-    f.template step<1>(mine.k, mine.v, LD, k0, w, rule, lane);
+    f.template step<1>(mine.k, mine.v, LD, LDV, k0, w, rule, lane);
     wave_sync();
   }
   if (w.hi <= w.lo) f.clear();
@@ -633,16 +680,36 @@ __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams 
   if (pair >= p.pairs) return;
   const size_t stride = (size_t)p.pairs * 32 * p.tiles * (p.D + 2);
   const float* o = p.part + ((size_t)pair * 32 * p.tiles + row) * (p.D + 2);
-  float top = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, o[s * stride + p.D]);
-  const float base = top == -INFINITY ? 0.0f : top;
-  float l = 0.0f, x[2] = {0.0f, 0.0f};
-  for (int s = 0; s < p.splits; ++s) {
-    const float a = __builtin_amdgcn_exp2f(o[s * stride + p.D] - base);
-    l = fmaf(a, o[s * stride + p.D + 1], l);
+  // Maxima and totals of 64 parts at a time, one a lane; then the sums, whose loads
+  // do not wait for each other.
+  float top = -INFINITY, l = 0.0f, x[2] = {0.0f, 0.0f};
+  for (int s0 = 0; s0 < p.splits; s0 += 64) {
+    const bool in = s0 + lane < p.splits;
+    const float m = in ? o[(s0 + lane) * stride + p.D] : -INFINITY;
+    float to = m;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (lane + 64 * e < p.D) x[e] = fmaf(a, o[s * stride + lane + 64 * e], x[e]);
+    for (int i = 1; i < 64; i *= 2) to = fmaxf(to, __shfl_xor(to, i));
+    to = fmaxf(top, to);
+    const float base = to == -INFINITY ? 0.0f : to, shrink = __builtin_amdgcn_exp2f(top - base);
+    const float a = __builtin_amdgcn_exp2f(m - base);
+    float part = in ? a * o[(s0 + lane) * stride + p.D + 1] : 0.0f;
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) part += __shfl_xor(part, i);
+    l = fmaf(l, shrink, part);
+    x[0] *= shrink;
+    x[1] *= shrink;
+    const int n = min(64, p.splits - s0);
+    for (int s = 0; s < n; s += 8) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = min(s + u, n - 1);
+        const float w = __shfl(a, i);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (lane + 64 * e < p.D && s + u < n) x[e] = fmaf(w, o[(s0 + i) * stride + lane + 64 * e], x[e]);
+      }
+    }
+    top = to;
   }
   const int tok = token_of(p, row), b = pair / p.Hk, h = pair % p.Hk * p.G + row - tok * p.G;
   T* out = head_out<T>(p.out, b, h) + (int64_t)tok * p.out.st;
@@ -654,10 +721,11 @@ __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams 
 }
 
 // ----------------------------------------------------------------- backward
-// Sums of the workgroup's four waves, in the first wave: two rounds through LDS.
-template <int N> __device__ __forceinline__ void add_waves(f32x16 (&x)[N], float* lds, int wave, int lane) {
+// Sums of W waves, number `wave` among them, in the first of them: rounds through
+// LDS (W / 2 times a wave's accumulators), which all waves of the workgroup make.
+template <int W, int N> __device__ __forceinline__ void add_waves(f32x16 (&x)[N], float* lds, int wave, int lane) {
 #pragma unroll
-  for (int from = kWaves / 2; from > 0; from /= 2) {
+  for (int from = W / 2; from > 0; from /= 2) {
     __syncthreads();
     if (wave >= from && wave < 2 * from) {
 #pragma unroll
@@ -686,21 +754,35 @@ template <class T, int DP> struct BackwardQ {
     for (int n = 0; n < NB; ++n, kt += 32 * ld, vt += 32 * ld, k0 += 32) {
       const Seen how = seen(w.lo, w.hi, k0, 32);
       if (how == Seen::none) continue;
-      f32x16 s(0.0f), dp(0.0f), bend(1.0f);
+      f32x16 s(0.0f), dp(0.0f);
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) s = mma(rows_frag(kt, ld, 16 * c, lane), q[c], s);
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) dp = mma(rows_frag(vt, ld, 16 * c, lane), g[c], dp);
-      score<T, true>(s, bend, rule, w.slope, w.at, k0, half);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = __builtin_amdgcn_exp2f(fmaf(s[r], rule.mul, -lse)) * (dp[r] - delta);
-        if (rule.capped) x *= bend[r];
-        if (how == Seen::some) {
-          const int key = k0 + acc_row(r, half);
-          x = key >= w.lo && key < w.hi ? x : 0.0f;
+      for (int r = 0; r < 16; ++r) dp[r] -= delta;
+      if (rule.capped) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = tanh_of<T>(s[r] * rule.pre);
+          dp[r] *= fmaf(-s[r], s[r], 1.0f);
         }
-        s[r] = x;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], rule.mul, -lse);
+      if (rule.sloped) {
+        const float d = (float)(w.at - k0 - 4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(-w.slope, fabsf(d - acc_row(r, 0)), s[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]) * dp[r];
+      if (how == Seen::some) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + acc_row(r, half);
+          s[r] = key >= w.lo && key < w.hi ? s[r] : 0.0f;
+        }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -719,7 +801,7 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
   constexpr int KT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
   __shared__ __align__(16) T kt[SETS][KT * LD];
   __shared__ __align__(16) T vt[SETS][KT * LD];
-  __shared__ int range[2 * kWaves];
+  __shared__ int range[2 * kMaxWaves];
   static_assert(!FEW || sizeof(kt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
   const Place at = place_of(p);
   if (at.idle) return;
@@ -758,29 +840,33 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
   const int first = keys.lo / KT * KT;
   if constexpr (FEW) {
     Stage<T, DP, 32, 64> ks, vs;
+    ks.init(p, p.k.st, lane);
+    vs.init(p, p.v.st, lane);
     int k0 = first + 32 * wave;
     if (k0 < keys.hi) {
-      ks.load(kb, p.k.st, k0, tk, p.D, p.vec, lane);
-      vs.load(vb, p.v.st, k0, tk, p.D, p.vec, lane);
+      ks.load(p, kb, p.k.st, k0, tk, lane);
+      vs.load(p, vb, p.v.st, k0, tk, lane);
     }
     for (; k0 < keys.hi; k0 += 32 * kWaves) {
       ks.store(kt[wave], LD, lane);
       vs.store(vt[wave], LD, lane);
       wave_sync();
       if (k0 + 32 * kWaves < keys.hi) {
-        ks.load(kb, p.k.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
-        vs.load(vb, p.v.st, k0 + 32 * kWaves, tk, p.D, p.vec, lane);
+        ks.load(p, kb, p.k.st, k0 + 32 * kWaves, tk, lane);
+        vs.load(p, vb, p.v.st, k0 + 32 * kWaves, tk, lane);
       }
       f.template step<1>(kt[wave], vt[wave], LD, k0, w, rule, lane);
       wave_sync();
     }
-    add_waves(f.dq, reinterpret_cast<float*>(kt), wave, lane);
+    add_waves<kWaves>(f.dq, reinterpret_cast<float*>(kt), wave, lane);
     if (wave > 0) return;
   } else {
     Stage<T, DP, KT, kThreads> ks, vs;
+    ks.init(p, p.k.st, tid);
+    vs.init(p, p.v.st, tid);
     if (first < keys.hi) {
-      ks.load(kb, p.k.st, first, tk, p.D, p.vec, tid);
-      vs.load(vb, p.v.st, first, tk, p.D, p.vec, tid);
+      ks.load(p, kb, p.k.st, first, tk, tid);
+      vs.load(p, vb, p.v.st, first, tk, tid);
       ks.store(kt[0], LD, tid);
       vs.store(vt[0], LD, tid);
     }
@@ -789,8 +875,8 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
     for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
       const bool more = k0 + KT < keys.hi;
       if (more) {
-        ks.load(kb, p.k.st, k0 + KT, tk, p.D, p.vec, tid);
-        vs.load(vb, p.v.st, k0 + KT, tk, p.D, p.vec, tid);
+        ks.load(p, kb, p.k.st, k0 + KT, tk, tid);
+        vs.load(p, vb, p.v.st, k0 + KT, tk, tid);
       }
       f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
       if (more) {
@@ -806,18 +892,18 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
 // What the rows of a tile bring along: the statistics and the keys they see.
 struct RowInfo {
   float lse, delta, slope;
-  int lo, hi, at;
+  int lo, hi, at;  // `at`: the token's place
 };
 template <int ROWS> struct RowTable {
-  float lse[ROWS], delta[ROWS], slope[ROWS];
-  int lo[ROWS], hi[ROWS], at[ROWS];
+  float lse[ROWS], delta[ROWS], slope[ROWS], at[ROWS];
+  int lo[ROWS], hi[ROWS];
   __device__ __forceinline__ void put(int i, const RowInfo& x) {
     lse[i] = x.lse;
     delta[i] = x.delta;
-    slope[i] = x.slope;
+    slope[i] = x.slope * kLog2E;
     lo[i] = x.lo;
     hi[i] = x.hi;
-    at[i] = x.at;
+    at[i] = (float)x.at;
   }
 };
 __device__ __forceinline__ RowInfo row_info(const AttnParams& p, int b, int hk, int row, int limit, int shift) {
@@ -831,7 +917,7 @@ __device__ __forceinline__ RowInfo row_info(const AttnParams& p, int b, int hk, 
     x.lo = see.x;
     x.hi = see.y;
     x.at = tok + shift;
-    x.slope = p.slope ? p.slope[hk * p.G + row - tok * p.G] * kLog2E : 0.0f;
+    if (p.slope) x.slope = p.slope[hk * p.G + row - tok * p.G];
   }
   return x;
 }
@@ -842,43 +928,59 @@ __device__ __forceinline__ RowInfo row_info(const AttnParams& p, int b, int hk, 
 template <class T, int DP> struct BackwardK {
   frag<T> k[DP / 16], v[DP / 16];
   f32x16 dk[DP / 32], dv[DP / 32];
-  // 32 rows in LDS against the keys from k0 on.
+  __device__ __forceinline__ void start(const AttnParams& p, int b, int hk, int key, int tk, int lane) {
+    const T* kr = head<T>(p.k, b, hk) + (int64_t)key * p.k.st;
+    const T* vr = head<T>(p.v, b, hk) + (int64_t)key * p.v.st;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+      k[c] = key < tk ? load_frag(kr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+      v[c] = key < tk ? load_frag(vr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+    }
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16(0.0f);
+  }
+  // Rows i0 ... i0 + 31 of a tile in LDS against the keys from k0 on.
   template <int ROWS> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int k0, const ScoreRule& rule, int lane) {
     const int half = lane / 32, key = k0 + lane % 32;
-    const Seen how = seen(t.lo[i0 + lane % 32], t.hi[i0 + lane % 32], k0, 32);
-    if (how == Seen::none) return;
+    const int lo = t.lo[i0 + lane % 32], hi = t.hi[i0 + lane % 32];
+    if (__ballot(lo < k0 + 32 && hi > k0) == 0) return;
     // Rows that see nothing have no statistics: they are masked, not taken for full.
-    const bool mask = __ballot(t.lo[i0 + lane % 32] <= k0 && t.hi[i0 + lane % 32] >= k0 + 32) != ~0ull;
+    const bool mask = __ballot(lo <= k0 && hi >= k0 + 32) != ~0ull;
+    qt += i0 * ld;
+    gt += i0 * ld;
     f32x16 s(0.0f), dp(0.0f);
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) s = mma(rows_frag(qt, ld, 16 * c, lane), k[c], s);
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dp = mma(rows_frag(gt, ld, 16 * c, lane), v[c], dp);
 #pragma unroll
-    for (int r4 = 0; r4 < 16; r4 += 4) {
-      const int i = i0 + acc_row(r4, half);
-      const f32x4 lse = *reinterpret_cast<const f32x4*>(&t.lse[i]), delta = *reinterpret_cast<const f32x4*>(&t.delta[i]);
+    for (int r = 0; r < 16; ++r) dp[r] -= t.delta[i0 + acc_row(r, half)];
+    if (rule.capped) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = r4 + e;
-        float x = s[r], bend = 1.0f;
-        if (rule.capped) {
-          const float y = tanh_of<T>(x * rule.scale);
-          x = y * rule.cap;
-          bend = fmaf(-y, y, 1.0f);
-        } else if (rule.mul == 1.0f) {
-          x *= rule.scale;
-        }
-        if (rule.sloped) x = fmaf(-t.slope[i + e], fabsf((float)(t.at[i + e] - key)), x);
-        float pr = __builtin_amdgcn_exp2f(fmaf(x, rule.mul, -lse[e]));
-        float ds = pr * (dp[r] - delta[e]) * bend;
-        if (mask) {
-          const bool sees = key >= t.lo[i + e] && key < t.hi[i + e];
-          pr = sees ? pr : 0.0f;
-          ds = sees ? ds : 0.0f;
-        }
-        s[r] = pr;
-        dp[r] = ds;
+      for (int r = 0; r < 16; ++r) {
+        s[r] = tanh_of<T>(s[r] * rule.pre);
+        dp[r] *= fmaf(-s[r], s[r], 1.0f);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], rule.mul, -t.lse[i0 + acc_row(r, half)]);
+    if (rule.sloped) {
+      const float at = (float)key;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(-t.slope[i0 + acc_row(r, half)], fabsf(t.at[i0 + acc_row(r, half)] - at), s[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(s[r]);
+      dp[r] *= s[r];
+    }
+    if (mask) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = i0 + acc_row(r, half);
+        const bool sees = key >= t.lo[i] && key < t.hi[i];
+        s[r] = sees ? s[r] : 0.0f;
+        dp[r] = sees ? dp[r] : 0.0f;
       }
     }
 #pragma unroll
@@ -893,31 +995,13 @@ template <class T, int DP> struct BackwardK {
   }
 };
 
-// FEW: 32 keys a workgroup, its waves take the blocks of 32 rows in turn; else
-// 128 keys a workgroup, 32 a wave, with shared tiles of rows.
-template <class T, int DP, bool FEW>
-__global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
-  constexpr int RT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
-  __shared__ __align__(16) T qt[SETS][RT * LD];
-  __shared__ __align__(16) T gt[SETS][RT * LD];
-  __shared__ __align__(16) RowTable<RT> table[SETS];
-  __shared__ int range[2 * kWaves];
-  static_assert(!FEW || sizeof(qt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
-  const Place at = place_of(p);
-  if (at.idle) return;
-  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
-  constexpr int KEYS = FEW ? 32 : 128;
-  const int kb0 = KEYS * at.tile, k0 = FEW ? kb0 : kb0 + 32 * wave;
-  const int key = k0 + lane % 32;
-  const bool in = key < p.Tk;
-  // The rows that see any of the workgroup's keys.
+// The rows that see any of the n keys from kb0 on.
+__device__ __forceinline__ Interval rows_seeing(const AttnParams& p, int b, int tq, int kb0, int n, int tk, int (&range)[2 * kMaxWaves]) {
   int lo = 0x7fffffff, hi = 0;
   if (kb0 < tk) {
-    for (int t = tid; t < tq; t += kThreads) {
+    for (int t = threadIdx.x; t < tq; t += blockDim.x) {
       const int2 s = p.see[(size_t)b * p.Tq + t];
-      if (s.x < kb0 + KEYS && s.y > kb0) {
+      if (s.x < kb0 + n && s.y > kb0) {
         lo = min(lo, t);
         hi = t + 1;
       }
@@ -926,75 +1010,126 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParam
   Interval rows = key_range(lo, hi, range);
   rows.lo *= p.G;
   rows.hi *= p.G;
+  return rows;
+}
+
+template <class T, int DP> __device__ __forceinline__ void store_keys(const AttnParams& p, int b, int hk, int key, const f32x16* dk, const f32x16* dv, int lane) {
+  if (key >= p.Tk) return;
+  store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, dk, p.scale, lane / 32, p.D, p.vec);
+  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, 1.0f, lane / 32, p.D, p.vec);
+}
+
+// Few keys, and fp32: 32 keys a workgroup, whose four waves take the blocks of 32
+// rows in turn; their sums are added at the end.
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
+  constexpr int LD = kLd<T, DP>;
+  // Products take so long in fp32 that the next tile need not be fetched meanwhile,
+  // for which there are no registers.
+  constexpr bool kAhead = sizeof(T) == 2;
+  __shared__ __align__(16) T qt[kWaves][32 * LD];
+  __shared__ __align__(16) T gt[kWaves][32 * LD];
+  __shared__ __align__(16) RowTable<32> table[kWaves];
+  __shared__ int range[2 * kMaxWaves];
+  static_assert(sizeof(qt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int k0 = 32 * at.tile, key = k0 + lane % 32;
+  const Interval rows = rows_seeing(p, b, tq, k0, 32, tk, range);
   const ScoreRule rule = score_rule(p);
-
   BackwardK<T, DP> f;
-  {
-    const T* kr = head<T>(p.k, b, hk) + (int64_t)key * p.k.st;
-    const T* vr = head<T>(p.v, b, hk) + (int64_t)key * p.v.st;
-#pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-      f.k[c] = key < tk ? load_frag(kr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
-      f.v[c] = key < tk ? load_frag(vr, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
-    }
-  }
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) f.dk[d] = f.dv[d] = f32x16(0.0f);
-
-  const int first = rows.lo / RT * RT, shift = tk - tq;
-  if constexpr (FEW) {
-    Stage<T, DP, 32, 64> qs, gs;
-    RowInfo info;
-    int r0 = first + 32 * wave;
-    const auto fetch = [&](int r) {
-      qs.load_rows(p, p.q, b, hk, r, rows.hi, lane);
-      gs.load_rows(p, p.dout, b, hk, r, rows.hi, lane);
-      if (lane < 32) info = row_info(p, b, hk, r + lane, rows.hi, shift);
-    };
-    if (r0 < rows.hi) fetch(r0);
-    for (; r0 < rows.hi; r0 += 32 * kWaves) {
+  f.start(p, b, hk, key, tk, lane);
+  Stage<T, DP, 32, 64> qs, gs;
+  qs.init_rows(p, p.q, lane);
+  gs.init_rows(p, p.dout, lane);
+  RowInfo info;
+  const auto fetch = [&](int r) {
+    if (lane < 32) info = row_info(p, b, hk, r + lane, rows.hi, tk - tq);
+    qs.load_rows(p, p.q, b, hk, r, tq * p.G, lane);
+    gs.load_rows(p, p.dout, b, hk, r, tq * p.G, lane);
+  };
+  int r0 = rows.lo / 32 * 32 + 32 * wave;
+  if (kAhead && r0 < rows.hi) fetch(r0);
+  for (; r0 < rows.hi; r0 += 32 * kWaves) {
+    if (kAhead) {
       qs.store(qt[wave], LD, lane);
       gs.store(gt[wave], LD, lane);
-      if (lane < 32) table[wave].put(lane, info);
-      wave_sync();
-      if (r0 + 32 * kWaves < rows.hi) fetch(r0 + 32 * kWaves);
-      f.step(qt[wave], gt[wave], LD, table[wave], 0, k0, rule, lane);
-      wave_sync();
+    } else {
+      if (lane < 32) info = row_info(p, b, hk, r0 + lane, rows.hi, tk - tq);
+      qs.load_rows(p, p.q, b, hk, r0, tq * p.G, lane);
+      qs.store(qt[wave], LD, lane);
+      gs.load_rows(p, p.dout, b, hk, r0, tq * p.G, lane);
+      gs.store(gt[wave], LD, lane);
     }
-    add_waves(f.dk, reinterpret_cast<float*>(qt), wave, lane);
-    add_waves(f.dv, reinterpret_cast<float*>(qt), wave, lane);
-    if (wave > 0) return;
-  } else {
-    Stage<T, DP, RT, kThreads> qs, gs;
-    RowInfo info;
-    const auto fetch = [&](int r) {
-      qs.load_rows(p, p.q, b, hk, r, rows.hi, tid);
-      gs.load_rows(p, p.dout, b, hk, r, rows.hi, tid);
-      if (tid < RT) info = row_info(p, b, hk, r + tid, rows.hi, shift);
-    };
-    const auto put = [&](int to) {
-      qs.store(qt[to], LD, tid);
-      gs.store(gt[to], LD, tid);
-      if (tid < RT) table[to].put(tid, info);
-    };
-    if (first < rows.hi) {
-      fetch(first);
-      put(0);
-    }
-    __syncthreads();
-    int cur = 0;
-    for (int r0 = first; r0 < rows.hi; r0 += RT, cur ^= 1) {
-      const bool more = r0 + RT < rows.hi;
-      if (more) fetch(r0 + RT);
-#pragma unroll
-      for (int n = 0; n < RT / 32; ++n) f.step(qt[cur] + 32 * n * LD, gt[cur] + 32 * n * LD, LD, table[cur], 32 * n, k0, rule, lane);
-      if (more) put(cur ^ 1);
-      __syncthreads();
-    }
+    if (lane < 32) table[wave].put(lane, info);
+    wave_sync();
+    if (kAhead && r0 + 32 * kWaves < rows.hi) fetch(r0 + 32 * kWaves);
+    f.step(qt[wave], gt[wave], LD, table[wave], 0, k0, rule, lane);
+    wave_sync();
   }
-  if (!in) return;
-  store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, f.dk, p.scale, lane / 32, p.D, p.vec);
-  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, f.dv, 1.0f, lane / 32, p.D, p.vec);
+  add_waves<kWaves>(f.dk, reinterpret_cast<float*>(qt), wave, lane);
+  add_waves<kWaves>(f.dv, reinterpret_cast<float*>(qt), wave, lane);
+  if (wave == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
+}
+
+// 16-bit types: 64 keys a workgroup, two waves by keys and two by rows, which
+// share tiles of 64 rows; the next tile is on its way while one is used.  Up to 64
+// channels two waves fit a SIMD, so that one multiplies while the other takes
+// exponents.
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_tiles(const AttnParams p) {
+  constexpr int LD = kLd<T, DP>, SUB = 1, RT = 64 * SUB;
+  __shared__ __align__(16) T tiles[2][2][RT * LD];
+  __shared__ __align__(16) RowTable<RT> table[2];
+  __shared__ int range[2 * kMaxWaves];
+  static_assert(sizeof(tiles) >= 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int by_key = wave % 2, by_row = wave / 2;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int kb0 = 64 * at.tile, k0 = kb0 + 32 * by_key, key = k0 + lane % 32;
+  BackwardK<T, DP> f;
+  f.start(p, b, hk, key, tk, lane);
+  const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
+  const ScoreRule rule = score_rule(p);
+  Stage<T, DP, RT, kThreads> qs, gs;
+  qs.init_rows(p, p.q, tid);
+  gs.init_rows(p, p.dout, tid);
+  RowInfo info;
+  const int first = rows.lo / 32 * 32, limit = tq * p.G;
+  const auto fetch = [&](int r) {
+    if (tid < RT) info = row_info(p, b, hk, r + tid, rows.hi, tk - tq);
+    qs.load_rows(p, p.q, b, hk, r, limit, tid);
+    gs.load_rows(p, p.dout, b, hk, r, limit, tid);
+  };
+  const auto put = [&](int to) {
+    qs.store(tiles[to][0], LD, tid);
+    gs.store(tiles[to][1], LD, tid);
+    if (tid < RT) table[to].put(tid, info);
+  };
+  if (first < rows.hi) {
+    fetch(first);
+    put(0);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int r0 = first; r0 < rows.hi; r0 += RT, cur ^= 1) {
+    const bool more = r0 + RT < rows.hi;
+    if (more) fetch(r0 + RT);
+#pragma unroll
+    for (int n = 0; n < SUB; ++n) f.step(tiles[cur][0], tiles[cur][1], LD, table[cur], 64 * n + 32 * by_row, k0, rule, lane);
+    if (more) put(cur ^ 1);
+    __syncthreads();
+  }
+  float* sums = reinterpret_cast<float*>(tiles) + by_key * ((DP / 32) * 16 * 64);
+  add_waves<2>(f.dk, sums, by_row, lane);
+  add_waves<2>(f.dv, sums, by_row, lane);
+  if (by_row == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
 }
 
 // Workgroups, and how place_of deals them out: over the dies if the last, partly
@@ -1031,14 +1166,18 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
     hipLaunchKernelGGL((mas_attention_dq<T, DP, false>), dim3(grid), dim3(kThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  p.tiles = (p.Tk + 127) / 128;
-  const bool few_keys = (int64_t)p.tiles * p.pairs < 256;
-  if (few_keys) p.tiles = (p.Tk + 31) / 32;
+  if constexpr (sizeof(T) == 2) {
+    // 64 keys a workgroup where those fill the compute units.
+    p.tiles = (p.Tk + 63) / 64;
+    if ((int64_t)p.tiles * p.pairs >= 256) {
+      grid = grid_of(p);
+      hipLaunchKernelGGL((mas_attention_dkv_tiles<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+      return hipGetLastError();
+    }
+  }
+  p.tiles = (p.Tk + 31) / 32;
   grid = grid_of(p);
-  if (few_keys)
-    hipLaunchKernelGGL((mas_attention_dkv<T, DP, true>), dim3(grid), dim3(kThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL((mas_attention_dkv<T, DP, false>), dim3(grid), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((mas_attention_dkv<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -1056,7 +1195,7 @@ AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk) {
   a.splits = 1;
   a.span = Tk;
   a.tiles = (rows + 127) / 128;
-  a.small = (int64_t)a.tiles * pairs < 256;
+  a.small = rows <= 32 || (int64_t)a.tiles * pairs < 256;
   if (!a.small) return a;
   a.tiles = (rows + 31) / 32;
   // Parts of at least 128 keys, a block for every wave, until two workgroups a

@@ -334,6 +334,7 @@ __global__ void __launch_bounds__(kThreads) mas_qk_weights_kernel(const QkParams
   const int col = threadIdx.x % 16, part = threadIdx.x / 16, c = (int)blockIdx.x * 16 + col;
   float x = 0.0f;
   if (c < 2 * p.D)
+#pragma unroll 8
     for (int i = part; i < blocks; i += 16) x += p.part[(size_t)i * 2 * p.D + c];
   sums[part][col] = x;
   __syncthreads();
