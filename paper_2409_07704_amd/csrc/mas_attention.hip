@@ -40,6 +40,7 @@ typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -200,73 +201,60 @@ template <class T> __device__ __forceinline__ frag<T> load_frag(const T* row, in
   return u.f;
 }
 
-// A tile of ROWS rows of DP channels on its way from memory to LDS, spread over
-// TEAM threads in 16-byte pieces.  Where the tile is inside the tensor, its rows are
-// whole pieces and its extent fits 32 bits, a piece's place in the tile is found
-// once and a tile costs one load each.
-template <class T, int DP, int ROWS, int TEAM> struct Stage {
+// Tiles of ROWS rows of DP channels on their way from memory to LDS, spread over
+// TEAM threads in 16-byte pieces: rows k of one head, st apart, or (BY_ROWS) rows of
+// the group's row axis.  Where a tile is inside the tensor, rows are whole aligned
+// pieces and the tile's extent fits 32 bits, a piece's place in the tile is found
+// once, and a tile costs one unconditional load each, which nothing waits for
+// before `store`.  Other tiles are fetched by `store`, element by element if need be.
+template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
   static constexpr int E = 16 / sizeof(T), CPR = DP / E, N = ROWS * CPR / TEAM;
   static_assert(ROWS * CPR % TEAM == 0, "whole pieces for every thread");
+  const AttnParams& p;
+  const HeadView& v;
+  const T* base;  // of the head, or of the group's first
+  int tid, limit; // zeros from row `limit` on
+  bool fast, whole;
+  int at;
   u32x4 r[N];
   uint32_t off[N];
-  bool fast;
-  static __device__ __forceinline__ int row(int n, int tid) { return (tid + n * TEAM) / CPR; }
-  static __device__ __forceinline__ int col(int n, int tid) { return (tid + n * TEAM) % CPR * E; }
-  // Rows of one head, st apart.
-  __device__ __forceinline__ void init(const AttnParams& p, int64_t st, int tid) {
-    fast = p.vec && st < (1 << 30) / (ROWS * (int)sizeof(T));
+  __device__ __forceinline__ int row(int n) const { return (tid + n * TEAM) / CPR; }
+  __device__ __forceinline__ int col(int n) const { return (tid + n * TEAM) % CPR * E; }
+  __device__ __forceinline__ Stage(const AttnParams& p, const HeadView& v, int b, int hk, int limit, int tid)
+      : p(p), v(v), base(head<T>(v, b, BY_ROWS ? hk * p.G : hk)), tid(tid), limit(limit), whole(false), at(0) {
+    const int most = (1 << 29) / (ROWS * (int)sizeof(T));
+    fast = p.vec && v.st < most && (!BY_ROWS || (32 % p.G == 0 && v.sh < most));
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      r[n] = u32x4(0);
-      off[n] = (uint32_t)(row(n, tid) * (int)st + col(n, tid)) * (uint32_t)sizeof(T);
+      const int i = row(n), c = col(n) < p.D ? col(n) : 0;
+      const int o = BY_ROWS ? (i >> p.g_shift) * (int)v.st + (i & (p.G - 1)) * (int)v.sh : i * (int)v.st;
+      off[n] = (uint32_t)(o + c) * (uint32_t)sizeof(T);
     }
   }
-  // Rows of the group's row axis, tiles of which start with a token.
-  __device__ __forceinline__ void init_rows(const AttnParams& p, const HeadView& v, int tid) {
-    fast = p.vec && 32 % p.G == 0 && v.st < (1 << 29) / (ROWS * (int)sizeof(T)) && v.sh < (1 << 29) / (ROWS * (int)sizeof(T));
+  // Rows from `k0` on (a multiple of 32) are wanted next.
+  __device__ __forceinline__ void load(int k0) {
+    at = k0;
+    whole = fast && k0 + ROWS <= limit;
+    if (!whole) return;
+    const char* tile = reinterpret_cast<const char*>(base + (int64_t)(BY_ROWS ? k0 >> p.g_shift : k0) * v.st);
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      r[n] = u32x4(0);
-      const int i = row(n, tid);
-      off[n] = (uint32_t)((i >> p.g_shift) * (int)v.st + (i & (p.G - 1)) * (int)v.sh + col(n, tid)) * (uint32_t)sizeof(T);
-    }
+    for (int n = 0; n < N; ++n) r[n] = *reinterpret_cast<const u32x4*>(tile + off[n]);
   }
-  __device__ __forceinline__ void load_whole(const void* tile, int D, int tid) {
+  __device__ __forceinline__ u32x4 slow(int i, int c) const {
+    if (i >= limit) return u32x4(0);
+    if (!BY_ROWS) return load16(base + (int64_t)i * v.st, c, p.D, p.vec);
+    const int tok = token_of(p, i);
+    return load16(base + (int64_t)(i - tok * p.G) * v.sh + (int64_t)tok * v.st, c, p.D, p.vec);
+  }
+  __device__ __forceinline__ void store(T* lds, int ld) const {
+    if (whole) {
+      const bool all = p.D == DP;
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-      if (col(n, tid) < D) r[n] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(tile) + off[n]);
-  }
-  // Rows k0 + i of a head; zeros from `limit` on.
-  __device__ __forceinline__ void load(const AttnParams& p, const T* base, int64_t st, int k0, int limit, int tid) {
-    if (fast && k0 + ROWS <= limit) return load_whole(base + k0 * st, p.D, tid);
+      for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n) * ld + col(n)) = all || col(n) < p.D ? r[n] : u32x4(0);
+    } else {
 #pragma unroll 1
-    for (int n = 0; n < N; ++n) {
-      const int i = k0 + row(n, tid);
-      const u32x4 x = i < limit ? load16(base + (int64_t)i * st, col(n, tid), p.D, p.vec) : u32x4(0);
-#pragma unroll
-      for (int m = 0; m < N; ++m)
-        if (m == n) r[m] = x;
+      for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n) * ld + col(n)) = slow(at + row(n), col(n));
     }
-  }
-  // Rows r0 + i of the group's row axis, r0 a multiple of 32.
-  __device__ __forceinline__ void load_rows(const AttnParams& p, const HeadView& v, int b, int hk, int r0, int limit, int tid) {
-    if (fast && r0 + ROWS <= limit) return load_whole(head<T>(v, b, hk * p.G) + (int64_t)(r0 >> p.g_shift) * v.st, p.D, tid);
-#pragma unroll 1
-    for (int n = 0; n < N; ++n) {
-      const int i = r0 + row(n, tid);
-      u32x4 x(0);
-      if (i < limit) {
-        const int tok = token_of(p, i);
-        x = load16(head<T>(v, b, hk * p.G + (i - tok * p.G)) + (int64_t)tok * v.st, col(n, tid), p.D, p.vec);
-      }
-#pragma unroll
-      for (int m = 0; m < N; ++m)
-        if (m == n) r[m] = x;
-    }
-  }
-  __device__ __forceinline__ void store(T* lds, int ld, int tid) const {
-#pragma unroll
-    for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n, tid) * ld + col(n, tid)) = r[n];
   }
 };
 
@@ -466,7 +454,7 @@ template <class T, int DP> struct Forward {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + 32 * n + acc_row(r, half);
-          s[n][r] = key >= w.lo && key < w.hi ? s[n][r] : -INFINITY;
+          s[n][r] = (key >= w.lo) & (key < w.hi) ? s[n][r] : -INFINITY;
         }
     }
     float top = s[0][0];
@@ -533,30 +521,26 @@ __global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnPara
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
   f.start();
 
-  const T* kb = head<T>(p.k, b, hk);
-  const T* vb = head<T>(p.v, b, hk);
-  Stage<T, DP, KT, kThreads> ks, vs;
-  ks.init(p, p.k.st, tid);
-  vs.init(p, p.v.st, tid);
+  Stage<T, DP, KT, kThreads, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
   const int first = keys.lo / KT * KT;
   if (first < keys.hi) {
-    ks.load(p, kb, p.k.st, first, tk, tid);
-    vs.load(p, vb, p.v.st, first, tk, tid);
-    ks.store(kt[0], LD, tid);
-    vs.store(vt[0], LDV, tid);
+    ks.load(first);
+    vs.load(first);
+    ks.store(kt[0], LD);
+    vs.store(vt[0], LDV);
   }
   __syncthreads();
   int cur = 0;
   for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
     const bool more = k0 + KT < keys.hi;
     if (more) {
-      ks.load(p, kb, p.k.st, k0 + KT, tk, tid);
-      vs.load(p, vb, p.v.st, k0 + KT, tk, tid);
+      ks.load(k0 + KT);
+      vs.load(k0 + KT);
     }
     f.template step<KT / 32>(kt[cur], vt[cur], LD, LDV, k0, w, rule, lane);
     if (more) {
-      ks.store(kt[cur ^ 1], LD, tid);
-      vs.store(vt[cur ^ 1], LDV, tid);
+      ks.store(kt[cur ^ 1], LD);
+      vs.store(vt[cur ^ 1], LDV);
     }
     __syncthreads();
   }
@@ -600,24 +584,20 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
   f.start();
 
-  const T* kb = head<T>(p.k, b, hk);
-  const T* vb = head<T>(p.v, b, hk);
-  Stage<T, DP, 32, 64> ks, vs;
-  ks.init(p, p.k.st, lane);
-  vs.init(p, p.v.st, lane);
+  Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
   Tiles& mine = lds.t[wave];
   int k0 = keys.lo + 32 * wave;
   if (k0 < keys.hi) {
-    ks.load(p, kb, p.k.st, k0, tk, lane);
-    vs.load(p, vb, p.v.st, k0, tk, lane);
+    ks.load(k0);
+    vs.load(k0);
   }
   for (; k0 < keys.hi; k0 += 32 * kWaves) {
-    ks.store(mine.k, LD, lane);
-    vs.store(mine.v, LDV, lane);
+    ks.store(mine.k, LD);
+    vs.store(mine.v, LDV);
     wave_sync();
     if (k0 + 32 * kWaves < keys.hi) {
-      ks.load(p, kb, p.k.st, k0 + 32 * kWaves, tk, lane);
-      vs.load(p, vb, p.v.st, k0 + 32 * kWaves, tk, lane);
+      ks.load(k0 + 32 * kWaves);
+      vs.load(k0 + 32 * kWaves);
     }
     f.template step<1>(mine.k, mine.v, LD, LDV, k0, w, rule, lane);
     wave_sync();
@@ -781,7 +761,7 @@ template <class T, int DP> struct BackwardQ {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + acc_row(r, half);
-          s[r] = key >= w.lo && key < w.hi ? s[r] : 0.0f;
+          s[r] = (key >= w.lo) & (key < w.hi) ? s[r] : 0.0f;
         }
       }
 #pragma unroll
@@ -835,25 +815,21 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) f.dq[d] = f32x16(0.0f);
 
-  const T* kb = head<T>(p.k, b, hk);
-  const T* vb = head<T>(p.v, b, hk);
   const int first = keys.lo / KT * KT;
   if constexpr (FEW) {
-    Stage<T, DP, 32, 64> ks, vs;
-    ks.init(p, p.k.st, lane);
-    vs.init(p, p.v.st, lane);
+    Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
     int k0 = first + 32 * wave;
     if (k0 < keys.hi) {
-      ks.load(p, kb, p.k.st, k0, tk, lane);
-      vs.load(p, vb, p.v.st, k0, tk, lane);
+      ks.load(k0);
+      vs.load(k0);
     }
     for (; k0 < keys.hi; k0 += 32 * kWaves) {
-      ks.store(kt[wave], LD, lane);
-      vs.store(vt[wave], LD, lane);
+      ks.store(kt[wave], LD);
+      vs.store(vt[wave], LD);
       wave_sync();
       if (k0 + 32 * kWaves < keys.hi) {
-        ks.load(p, kb, p.k.st, k0 + 32 * kWaves, tk, lane);
-        vs.load(p, vb, p.v.st, k0 + 32 * kWaves, tk, lane);
+        ks.load(k0 + 32 * kWaves);
+        vs.load(k0 + 32 * kWaves);
       }
       f.template step<1>(kt[wave], vt[wave], LD, k0, w, rule, lane);
       wave_sync();
@@ -861,27 +837,25 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
     add_waves<kWaves>(f.dq, reinterpret_cast<float*>(kt), wave, lane);
     if (wave > 0) return;
   } else {
-    Stage<T, DP, KT, kThreads> ks, vs;
-    ks.init(p, p.k.st, tid);
-    vs.init(p, p.v.st, tid);
+    Stage<T, DP, KT, kThreads, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
     if (first < keys.hi) {
-      ks.load(p, kb, p.k.st, first, tk, tid);
-      vs.load(p, vb, p.v.st, first, tk, tid);
-      ks.store(kt[0], LD, tid);
-      vs.store(vt[0], LD, tid);
+      ks.load(first);
+      vs.load(first);
+      ks.store(kt[0], LD);
+      vs.store(vt[0], LD);
     }
     __syncthreads();
     int cur = 0;
     for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
       const bool more = k0 + KT < keys.hi;
       if (more) {
-        ks.load(p, kb, p.k.st, k0 + KT, tk, tid);
-        vs.load(p, vb, p.v.st, k0 + KT, tk, tid);
+        ks.load(k0 + KT);
+        vs.load(k0 + KT);
       }
       f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
       if (more) {
-        ks.store(kt[cur ^ 1], LD, tid);
-        vs.store(vt[cur ^ 1], LD, tid);
+        ks.store(kt[cur ^ 1], LD);
+        vs.store(vt[cur ^ 1], LD);
       }
       __syncthreads();
     }
@@ -889,38 +863,36 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_a
   if (w.in) store_row<T, DP>(head_out<T>(p.dq, b, w.h) + (int64_t)w.tok * p.dq.st, f.dq, w.hi > w.lo ? p.scale : 0.0f, lane / 32, p.D, p.vec);
 }
 
-// What the rows of a tile bring along: the statistics and the keys they see.
+// What a row brings along: its statistics and the keys it sees.  Loaded without
+// conditions (rows past the end load the last one's), put to use by `put`.
 struct RowInfo {
-  float lse, delta, slope;
-  int lo, hi, at;  // `at`: the token's place
+  float2 stat;
+  int2 see;
+  float slope;
+  int row, tok;
+  __device__ __forceinline__ void load(const AttnParams& p, int b, int hk, int r) {
+    row = r;
+    const int i = min(r, p.rows - 1);
+    tok = token_of(p, i);
+    stat = p.stat[((size_t)b * p.Hk + hk) * p.rows + i];
+    see = p.see[(size_t)b * p.Tq + tok];
+    slope = p.slope ? p.slope[hk * p.G + i - tok * p.G] : 0.0f;
+  }
 };
 template <int ROWS> struct RowTable {
   float lse[ROWS], delta[ROWS], slope[ROWS], at[ROWS];
   int lo[ROWS], hi[ROWS];
-  __device__ __forceinline__ void put(int i, const RowInfo& x) {
-    lse[i] = x.lse;
-    delta[i] = x.delta;
+  // shift: from a token to its place; rows from `limit` on see nothing.
+  __device__ __forceinline__ void put(int i, const RowInfo& x, int shift, int limit) {
+    lse[i] = x.stat.x;
+    delta[i] = x.stat.y;
     slope[i] = x.slope * kLog2E;
-    lo[i] = x.lo;
-    hi[i] = x.hi;
-    at[i] = (float)x.at;
+    at[i] = (float)(x.tok + shift);
+    lo[i] = x.row < limit ? x.see.x : 0;
+    hi[i] = x.row < limit ? x.see.y : 0;
   }
 };
-__device__ __forceinline__ RowInfo row_info(const AttnParams& p, int b, int hk, int row, int limit, int shift) {
-  RowInfo x = {0.0f, 0.0f, 0.0f, 0, 0, 0};
-  if (row < limit) {
-    const int tok = token_of(p, row);
-    const float2 s = p.stat[((size_t)b * p.Hk + hk) * p.rows + row];
-    const int2 see = p.see[(size_t)b * p.Tq + tok];
-    x.lse = s.x;
-    x.delta = s.y;
-    x.lo = see.x;
-    x.hi = see.y;
-    x.at = tok + shift;
-    if (p.slope) x.slope = p.slope[hk * p.G + row - tok * p.G];
-  }
-  return x;
-}
+template <class V> __device__ __forceinline__ V four_at(const void* at) { return *reinterpret_cast<const V*>(at); }
 
 // dk, dv of a wave's 32 keys (lane l and l + 32 hold key l % 32): s = q k^T with
 // the rows down the registers, so that p and ds are operands of dv^T = dout^T p
@@ -949,12 +921,24 @@ template <class T, int DP> struct BackwardK {
     qt += i0 * ld;
     gt += i0 * ld;
     f32x16 s(0.0f), dp(0.0f);
+    {
+      frag<T> x[DP / 16];
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) s = mma(rows_frag(qt, ld, 16 * c, lane), k[c], s);
+      for (int c = 0; c < DP / 16; ++c) x[c] = rows_frag(qt, ld, 16 * c, lane);
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) dp = mma(rows_frag(gt, ld, 16 * c, lane), v[c], dp);
+      for (int c = 0; c < DP / 16; ++c) s = mma(x[c], k[c], s);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] -= t.delta[i0 + acc_row(r, half)];
+      for (int c = 0; c < DP / 16; ++c) x[c] = rows_frag(gt, ld, 16 * c, lane);
+#pragma unroll
+      for (int c = 0; c < DP / 16; ++c) dp = mma(x[c], v[c], dp);
+    }
+    const int i = i0 + 4 * half;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const f32x4 delta = four_at<f32x4>(&t.delta[i + 2 * r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[r + e] -= delta[e];
+    }
     if (rule.capped) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -963,11 +947,19 @@ template <class T, int DP> struct BackwardK {
       }
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], rule.mul, -t.lse[i0 + acc_row(r, half)]);
-    if (rule.sloped) {
-      const float at = (float)key;
+    for (int r = 0; r < 16; r += 4) {
+      const f32x4 lse = four_at<f32x4>(&t.lse[i + 2 * r]);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(-t.slope[i0 + acc_row(r, half)], fabsf(t.at[i0 + acc_row(r, half)] - at), s[r]);
+      for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, -lse[e]);
+    }
+    if (rule.sloped) {
+      const float place = (float)key;
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const f32x4 slope = four_at<f32x4>(&t.slope[i + 2 * r]), at = four_at<f32x4>(&t.at[i + 2 * r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[r + e] = fmaf(-slope[e], fabsf(at[e] - place), s[r + e]);
+      }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -976,11 +968,14 @@ template <class T, int DP> struct BackwardK {
     }
     if (mask) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int i = i0 + acc_row(r, half);
-        const bool sees = key >= t.lo[i] && key < t.hi[i];
-        s[r] = sees ? s[r] : 0.0f;
-        dp[r] = sees ? dp[r] : 0.0f;
+      for (int r = 0; r < 16; r += 4) {
+        const i32x4 from = four_at<i32x4>(&t.lo[i + 2 * r]), to = four_at<i32x4>(&t.hi[i + 2 * r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool sees = (key >= from[e]) & (key < to[e]);
+          s[r + e] = sees ? s[r + e] : 0.0f;
+          dp[r + e] = sees ? dp[r + e] : 0.0f;
+        }
       }
     }
 #pragma unroll
@@ -1042,29 +1037,27 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParam
   const ScoreRule rule = score_rule(p);
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
-  Stage<T, DP, 32, 64> qs, gs;
-  qs.init_rows(p, p.q, lane);
-  gs.init_rows(p, p.dout, lane);
+  Stage<T, DP, 32, 64, true> qs(p, p.q, b, hk, tq * p.G, lane), gs(p, p.dout, b, hk, tq * p.G, lane);
   RowInfo info;
   const auto fetch = [&](int r) {
-    if (lane < 32) info = row_info(p, b, hk, r + lane, rows.hi, tk - tq);
-    qs.load_rows(p, p.q, b, hk, r, tq * p.G, lane);
-    gs.load_rows(p, p.dout, b, hk, r, tq * p.G, lane);
+    info.load(p, b, hk, r + lane % 32);
+    qs.load(r);
+    gs.load(r);
   };
   int r0 = rows.lo / 32 * 32 + 32 * wave;
   if (kAhead && r0 < rows.hi) fetch(r0);
   for (; r0 < rows.hi; r0 += 32 * kWaves) {
     if (kAhead) {
-      qs.store(qt[wave], LD, lane);
-      gs.store(gt[wave], LD, lane);
+      qs.store(qt[wave], LD);
+      gs.store(gt[wave], LD);
     } else {
-      if (lane < 32) info = row_info(p, b, hk, r0 + lane, rows.hi, tk - tq);
-      qs.load_rows(p, p.q, b, hk, r0, tq * p.G, lane);
-      qs.store(qt[wave], LD, lane);
-      gs.load_rows(p, p.dout, b, hk, r0, tq * p.G, lane);
-      gs.store(gt[wave], LD, lane);
+      info.load(p, b, hk, r0 + lane % 32);
+      qs.load(r0);
+      qs.store(qt[wave], LD);
+      gs.load(r0);
+      gs.store(gt[wave], LD);
     }
-    if (lane < 32) table[wave].put(lane, info);
+    if (lane < 32) table[wave].put(lane, info, tk - tq, rows.hi);
     wave_sync();
     if (kAhead && r0 + 32 * kWaves < rows.hi) fetch(r0 + 32 * kWaves);
     f.step(qt[wave], gt[wave], LD, table[wave], 0, k0, rule, lane);
@@ -1097,20 +1090,18 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   f.start(p, b, hk, key, tk, lane);
   const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
   const ScoreRule rule = score_rule(p);
-  Stage<T, DP, RT, kThreads> qs, gs;
-  qs.init_rows(p, p.q, tid);
-  gs.init_rows(p, p.dout, tid);
+  Stage<T, DP, RT, kThreads, true> qs(p, p.q, b, hk, tq * p.G, tid), gs(p, p.dout, b, hk, tq * p.G, tid);
   RowInfo info;
-  const int first = rows.lo / 32 * 32, limit = tq * p.G;
+  const int first = rows.lo / 32 * 32;
   const auto fetch = [&](int r) {
-    if (tid < RT) info = row_info(p, b, hk, r + tid, rows.hi, tk - tq);
-    qs.load_rows(p, p.q, b, hk, r, limit, tid);
-    gs.load_rows(p, p.dout, b, hk, r, limit, tid);
+    info.load(p, b, hk, r + tid % RT);
+    qs.load(r);
+    gs.load(r);
   };
   const auto put = [&](int to) {
-    qs.store(tiles[to][0], LD, tid);
-    gs.store(tiles[to][1], LD, tid);
-    if (tid < RT) table[to].put(tid, info);
+    qs.store(tiles[to][0], LD);
+    gs.store(tiles[to][1], LD);
+    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi);
   };
   if (first < rows.hi) {
     fetch(first);
