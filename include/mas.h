@@ -302,7 +302,9 @@ typedef struct mas_heads {
  *   kernels access memory outside the tensors, but results are unspecified.
  * A query that sees no key (and every query past t_q) gets zeros, log-sum-exp
  * -inf and no gradient.  Padding of the inputs never influences a result,
- * whatever it holds.
+ * whatever it holds; nor does a hidden key or value influence `out` and the
+ * log-sum-exp, infinities and NaN included.  (In the backward pass, an infinity
+ * or NaN inside the lengths may reach gradients of its neighbours.)
  * Precision: sums, maxima and totals in fp32; in the 16-bit types p and ds are
  * rounded to the type before they are multiplied (fp16: as for its gradients
  * at large, values below 6e-8 are lost, so scale the loss); results are

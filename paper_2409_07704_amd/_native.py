@@ -304,30 +304,45 @@ def mas_forward(value, t_x, t_y, path_out=None, stream=None):
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-def _heads(t, name, like=None, shape=None):
-    """mas_heads of a tensor [B, T, H, D] with contiguous channels."""
+def _heads(t, name, like, shape):
+    """mas_heads of a tensor [B, T, H, D] with contiguous channels, of the type,
+    device and shape that the call's other tensors ask for."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device (cuda/hip) tensor")
-    if t.dtype not in _DTYPES or (like is not None and t.dtype != like.dtype):
-        raise TypeError(f"{name} must be {like.dtype if like is not None else 'float32, float16 or bfloat16'}, got {t.dtype}")
-    if like is not None and t.device != like.device:
+    if t.dtype is not like.dtype or t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be {like.dtype if t is not like else 'float32, float16 or bfloat16'}, got {t.dtype}")
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} must be on {like.device}, got {t.device}")
-    if t.dim() != 4:
-        raise ValueError(f"{name} must be [B, T, H, D]")
-    if shape is not None and t.shape != torch.Size(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     sb, st, sh, sd = t.stride()
-    if sd != 1 and t.shape[3] > 1:
+    if sd != 1 and shape[3] > 1:
         raise ValueError(f"{name} must have contiguous channels")
     return Heads(t.data_ptr(), sb, st, sh)
 
 
-def _arg(t, name, dtype, shape, device):
+def _arg(t, name, dtype, shape, like):
     """Pointer of an optional contiguous tensor on the call's device."""
-    p = _dev_ptr(t, name, dtype, shape)
-    if t is not None and t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    return p
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device (cuda/hip) tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _run_on(stream, like):
+    """The call's stream as a handle."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(like.get_device())
+    return _stream(stream, like.device)
 
 
 def _on(stream, device):
@@ -341,17 +356,16 @@ def _on(stream, device):
     return torch.cuda.stream(stream)
 
 
-def _scratch(workspace, nbytes, device, stream):
-    """(pointer, bytes) of the caller's uint8 workspace, or of a new one, and what
-    keeps it alive until the call is enqueued."""
-    if nbytes == 0:
-        raise ValueError("invalid shape")
-    if workspace is None:
-        with _on(stream, device):
-            workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
-        off = -workspace.data_ptr() % 256
-        return workspace.data_ptr() + off, nbytes, workspace
-    return _arg(workspace, "workspace", torch.uint8, None, device), workspace.numel(), workspace
+def _scratch(workspace, nbytes, like, stream):
+    """(pointer, bytes) of the caller's uint8 workspace, or of a new one of
+    nbytes() (0 for a shape that the call will refuse), and what keeps it alive
+    until the call is enqueued."""
+    if workspace is not None:
+        return _arg(workspace, "workspace", torch.uint8, None, like), workspace.numel(), workspace
+    n = int(nbytes())
+    with _on(stream, like.device):
+        workspace = torch.empty(n + 256, dtype=torch.uint8, device=like.device)
+    return workspace.data_ptr() + -workspace.data_ptr() % 256, n, workspace
 
 
 def _empty(shape, dtype, device, stream):
@@ -360,11 +374,10 @@ def _empty(shape, dtype, device, stream):
 
 
 def _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix):
-    if q.dim() != 4 or k.dim() != 4:
+    if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or q.dim() != 4 or k.dim() != 4:
         raise ValueError("q must be [B, Tq, Hq, D] and k [B, Tk, Hk, D]")
     B, Tq, Hq, D = q.shape
-    Tk, Hk = k.shape[1], k.shape[2]
-    dev = q.device
+    _, Tk, Hk, _ = k.shape
     N = 1
     if doc_start is not None:
         if doc_start.dim() != 2:
@@ -372,16 +385,16 @@ def _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix
         N = doc_start.shape[1] - 1
     return AttentionDesc(B, Tq, Tk, Hq, Hk, D, _DTYPES.get(q.dtype, -1), 1 if causal else 0, N,
                          1.0 / math.sqrt(max(D, 1)) if scale is None else scale, cap,
-                         _arg(t_q, "t_q", torch.int32, (B,), dev), _arg(t_k, "t_k", torch.int32, (B,), dev),
-                         _arg(slope, "slope", torch.float32, (Hq,), dev),
-                         _arg(doc_start, "doc_start", torch.int32, (B, N + 1), dev),
-                         _arg(prefix, "prefix", torch.int32, (B, N), dev))
+                         _arg(t_q, "t_q", torch.int32, (B,), q), _arg(t_k, "t_k", torch.int32, (B,), q),
+                         _arg(slope, "slope", torch.float32, (Hq,), q),
+                         _arg(doc_start, "doc_start", torch.int32, (B, N + 1), q),
+                         _arg(prefix, "prefix", torch.int32, (B, N), q)), (B, Tk, Hk, D)
 
 
 def mas_attention_workspace_bytes(q, k, backward: bool = False) -> int:
     """Bytes of workspace for mas_attention of q [B, Tq, Hq, D] over k [B, Tk,
     Hk, D] and, with `backward`, for mas_attention_backward too."""
-    d = _attention_desc(q, k, None, None, False, None, 0.0, None, None, None)
+    d, _ = _attention_desc(q, k, None, None, False, None, 0.0, None, None, None)
     return int(lib().mas_attention_workspace_bytes(d, 1 if backward else 0))
 
 
@@ -396,16 +409,15 @@ def mas_attention(q, k, v, t_q=None, t_k=None, causal=False, scale=None, cap=0.0
     and prefix [B, N] int32: see mas.h.  lse_out [B, Hq, Tq] fp32 is what the
     backward pass takes.  workspace: a uint8 tensor of
     mas_attention_workspace_bytes, 256-byte aligned, or None."""
-    d = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
-    hq, hk = _heads(q, "q"), _heads(k, "k", q, (d.B, d.Tk, d.Hk, d.D))
-    hv = _heads(v, "v", q, (d.B, d.Tk, d.Hk, d.D))
+    d, kv = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
+    hq, hk, hv = _heads(q, "q", q, q.shape), _heads(k, "k", q, kv), _heads(v, "v", q, kv)
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
     ho = _heads(out, "out", q, q.shape)
-    pl = _arg(lse_out, "lse_out", torch.float32, (d.B, d.Hq, d.Tq), q.device)
+    pl = _arg(lse_out, "lse_out", torch.float32, (d.B, d.Hq, d.Tq), q)
     L = lib()
-    ws, n, keep = _scratch(workspace, L.mas_attention_workspace_bytes(d, 0) if workspace is None else 1, q.device, stream)
-    _check("mas_attention", L.mas_attention(d, hq, hk, hv, ho, pl, ws, n, _stream(stream, q.device)))
+    ws, n, keep = _scratch(workspace, lambda: L.mas_attention_workspace_bytes(d, 0), q, stream)
+    _check("mas_attention", L.mas_attention(d, hq, hk, hv, ho, pl, ws, n, _run_on(stream, q)))
     return out
 
 
@@ -413,36 +425,35 @@ def mas_attention_backward(dout, q, k, v, out, lse, t_q=None, t_k=None, causal=F
                            doc_start=None, prefix=None, dq=None, dk=None, dv=None, workspace=None, stream=None):
     """Gradients (dq, dk, dv) of mas_attention from dout [B, Tq, Hq, D], the
     inputs, and the forward call's out and lse_out; other arguments as there."""
-    d = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
-    kv = (d.B, d.Tk, d.Hk, d.D)
-    hq, hk, hv = _heads(q, "q"), _heads(k, "k", q, kv), _heads(v, "v", q, kv)
+    d, kv = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
+    hq, hk, hv = _heads(q, "q", q, q.shape), _heads(k, "k", q, kv), _heads(v, "v", q, kv)
     ho, hg = _heads(out, "out", q, q.shape), _heads(dout, "dout", q, q.shape)
     if lse is None:
         raise TypeError("lse must be a device (cuda/hip) tensor")
-    pl = _arg(lse, "lse", torch.float32, (d.B, d.Hq, d.Tq), q.device)
+    pl = _arg(lse, "lse", torch.float32, (d.B, d.Hq, d.Tq), q)
     dq = _empty(q.shape, q.dtype, q.device, stream) if dq is None else dq
     dk = _empty(kv, q.dtype, q.device, stream) if dk is None else dk
     dv = _empty(kv, q.dtype, q.device, stream) if dv is None else dv
     gq, gk, gv = _heads(dq, "dq", q, q.shape), _heads(dk, "dk", q, kv), _heads(dv, "dv", q, kv)
     L = lib()
-    ws, n, keep = _scratch(workspace, L.mas_attention_workspace_bytes(d, 1) if workspace is None else 1, q.device, stream)
+    ws, n, keep = _scratch(workspace, lambda: L.mas_attention_workspace_bytes(d, 1), q, stream)
     _check("mas_attention_backward",
-           L.mas_attention_backward(d, hg, hq, hk, hv, ho, pl, gq, gk, gv, ws, n, _stream(stream, q.device)))
+           L.mas_attention_backward(d, hg, hq, hk, hv, ho, pl, gq, gk, gv, ws, n, _run_on(stream, q)))
     return dq, dk, dv
 
 
 def _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved):
-    if q.dim() != 4 or (k is not None and k.dim() != 4):
+    if not isinstance(q, torch.Tensor) or q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q must be [B, T, Hq, D] and k [B, T, Hk, D] or None")
     B, T, Hq, D = q.shape
-    Hk, dev = 0 if k is None else k.shape[2], q.device
+    Hk = 0 if k is None else k.shape[2]
     if (cos is None) != (sin is None) or (cos is not None and cos.dim() != 2):
         raise ValueError("cos and sin must both be [P, R / 2], or None")
     P, half = (0, 0) if cos is None else cos.shape
     return QkDesc(B, T, Hq, Hk, D, 2 * half, P, _DTYPES.get(q.dtype, -1), 1 if interleaved else 0, eps,
-                  _arg(wq, "wq", torch.float32, (D,), dev), _arg(wk, "wk", torch.float32, (D,), dev),
-                  _arg(cos, "cos", torch.float32, (P, half), dev), _arg(sin, "sin", torch.float32, (P, half), dev),
-                  _arg(pos, "pos", torch.int32, (B, T), dev), _arg(t_x, "t_x", torch.int32, (B,), dev))
+                  _arg(wq, "wq", torch.float32, (D,), q), _arg(wk, "wk", torch.float32, (D,), q),
+                  _arg(cos, "cos", torch.float32, (P, half), q), _arg(sin, "sin", torch.float32, (P, half), q),
+                  _arg(pos, "pos", torch.int32, (B, T), q), _arg(t_x, "t_x", torch.int32, (B,), q)), (B, T, Hk, D)
 
 
 def mas_qk_norm_rope(q, k, wq, wk, cos, sin, pos=None, t_x=None, eps=1e-6, interleaved=False, q_out=None, k_out=None,
@@ -452,15 +463,16 @@ def mas_qk_norm_rope(q, k, wq, wk, cos, sin, pos=None, t_x=None, eps=1e-6, inter
     R channels by the rows pos [B, T] int32 (None: the token's index) of cos,
     sin [P, R / 2] fp32; returns (q_out, k_out).  Padding (t >= t_x) becomes
     zeros.  q_out, k_out may be q, k."""
-    d = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
-    ks = None if k is None else (d.B, d.T, d.Hk, d.D)
-    hq, hk = _heads(q, "q"), None if k is None else _heads(k, "k", q, ks)
+    d, ks = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
+    hq, hk = _heads(q, "q", q, q.shape), None if k is None else _heads(k, "k", q, ks)
     q_out = _empty(q.shape, q.dtype, q.device, stream) if q_out is None else q_out
-    if k is not None and k_out is None:
+    if k is None:
+        k_out = None
+    elif k_out is None:
         k_out = _empty(ks, q.dtype, q.device, stream)
     oq, ok = _heads(q_out, "q_out", q, q.shape), None if k is None else _heads(k_out, "k_out", q, ks)
-    _check("mas_qk_norm_rope", lib().mas_qk_norm_rope(d, hq, hk, oq, ok, _stream(stream, q.device)))
-    return q_out, k_out if k is not None else None
+    _check("mas_qk_norm_rope", lib().mas_qk_norm_rope(d, hq, hk, oq, ok, _run_on(stream, q)))
+    return q_out, k_out
 
 
 def mas_qk_norm_rope_workspace_bytes(q, k) -> int:
@@ -473,22 +485,23 @@ def mas_qk_norm_rope_backward(dq_out, dk_out, q, k, wq, wk, cos, sin, pos=None, 
                               dq=None, dk=None, dwq=None, dwk=None, workspace=None, stream=None):
     """Gradients (dq, dk, dwq, dwk) of mas_qk_norm_rope from those of its
     outputs and its inputs; dwq, dwk [D] fp32.  dk, dwk are None without k."""
-    d = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
-    dev, ks = q.device, None if k is None else (d.B, d.T, d.Hk, d.D)
-    hq, hk = _heads(q, "q"), None if k is None else _heads(k, "k", q, ks)
+    d, ks = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
+    hq, hk = _heads(q, "q", q, q.shape), None if k is None else _heads(k, "k", q, ks)
     gq, gk = _heads(dq_out, "dq_out", q, q.shape), None if k is None else _heads(dk_out, "dk_out", q, ks)
-    dq = _empty(q.shape, q.dtype, dev, stream) if dq is None else dq
-    dwq = _empty((d.D,), torch.float32, dev, stream) if dwq is None else dwq
-    if k is not None:
-        dk = _empty(ks, q.dtype, dev, stream) if dk is None else dk
-        dwk = _empty((d.D,), torch.float32, dev, stream) if dwk is None else dwk
+    dq = _empty(q.shape, q.dtype, q.device, stream) if dq is None else dq
+    dwq = _empty((d.D,), torch.float32, q.device, stream) if dwq is None else dwq
+    if k is None:
+        dk = dwk = None
+    else:
+        dk = _empty(ks, q.dtype, q.device, stream) if dk is None else dk
+        dwk = _empty((d.D,), torch.float32, q.device, stream) if dwk is None else dwk
     oq, ok = _heads(dq, "dq", q, q.shape), None if k is None else _heads(dk, "dk", q, ks)
-    pq = _arg(dwq, "dwq", torch.float32, (d.D,), dev)
-    pk = None if k is None else _arg(dwk, "dwk", torch.float32, (d.D,), dev)
-    ws, n, keep = _scratch(workspace, mas_qk_norm_rope_workspace_bytes(q, k) if workspace is None else 1, dev, stream)
+    pq, pk = _arg(dwq, "dwq", torch.float32, (d.D,), q), _arg(dwk, "dwk", torch.float32, (d.D,), q)
+    L = lib()
+    ws, n, keep = _scratch(workspace, lambda: L.mas_qk_norm_rope_workspace_bytes(d.B, d.T, d.Hq, d.Hk, d.D), q, stream)
     _check("mas_qk_norm_rope_backward",
-           lib().mas_qk_norm_rope_backward(d, gq, gk, hq, hk, oq, ok, pq, pk, ws, n, _stream(stream, dev)))
-    return (dq, dk, dwq, dwk) if k is not None else (dq, None, dwq, None)
+           L.mas_qk_norm_rope_backward(d, gq, gk, hq, hk, oq, ok, pq, pk, ws, n, _run_on(stream, q)))
+    return dq, dk, dwq, dwk
 
 
 def mas_align_loss_workspace_bytes(B: int, T: int, S: int, D: int) -> int:
@@ -503,25 +516,26 @@ def mas_align_loss(mu, log_sigma, z, row_start, item_weight=None, loss_out=None,
     item_weight [B] (None: 1); returns (loss, dmu, dlog_sigma, dz).  dlog_sigma
     is None without log_sigma unless given; without `gradients` only those given
     are made."""
-    if mu.dim() != 3 or z.dim() != 3:
+    if not isinstance(mu, torch.Tensor) or mu.dim() != 3 or z.dim() != 3:
         raise ValueError("mu must be [B, T, D] and z [B, S, D]")
     B, T, D = mu.shape
-    S, dev = z.shape[1], mu.device
-    f32 = torch.float32
-    pm, pl = _dev_ptr(mu, "mu", f32), _arg(log_sigma, "log_sigma", f32, (B, T, D), dev)
-    pz = _arg(z, "z", f32, (B, S, D), dev)
-    pr = _arg(row_start, "row_start", torch.int32, (B, T + 1), dev)
-    pw = _arg(item_weight, "item_weight", f32, (B,), dev)
-    loss_out = _empty((B,), f32, dev, stream) if loss_out is None else loss_out
+    S, f32 = z.shape[1], torch.float32
+    pm, pl = _arg(mu, "mu", f32, mu.shape, mu), _arg(log_sigma, "log_sigma", f32, mu.shape, mu)
+    pz = _arg(z, "z", f32, (B, S, D), mu)
+    pr = _arg(row_start, "row_start", torch.int32, (B, T + 1), mu)
+    pw = _arg(item_weight, "item_weight", f32, (B,), mu)
+    if pz is None or pr is None:
+        raise TypeError("z and row_start must be device (cuda/hip) tensors")
+    loss_out = _empty((B,), f32, mu.device, stream) if loss_out is None else loss_out
     if gradients:
-        dmu = _empty((B, T, D), f32, dev, stream) if dmu is None else dmu
-        dz = _empty((B, S, D), f32, dev, stream) if dz is None else dz
+        dmu = _empty((B, T, D), f32, mu.device, stream) if dmu is None else dmu
+        dz = _empty((B, S, D), f32, mu.device, stream) if dz is None else dz
         if dlog_sigma is None and log_sigma is not None:
-            dlog_sigma = _empty((B, T, D), f32, dev, stream)
-    po = _arg(loss_out, "loss_out", f32, (B,), dev)
-    gm, gl = _arg(dmu, "dmu", f32, (B, T, D), dev), _arg(dlog_sigma, "dlog_sigma", f32, (B, T, D), dev)
-    gz = _arg(dz, "dz", f32, (B, S, D), dev)
+            dlog_sigma = _empty((B, T, D), f32, mu.device, stream)
+    po = _arg(loss_out, "loss_out", f32, (B,), mu)
+    gm, gl = _arg(dmu, "dmu", f32, mu.shape, mu), _arg(dlog_sigma, "dlog_sigma", f32, mu.shape, mu)
+    gz = _arg(dz, "dz", f32, (B, S, D), mu)
     L = lib()
-    ws, n, keep = _scratch(workspace, L.mas_align_loss_workspace_bytes(B, T, S, D) if workspace is None else 1, dev, stream)
-    _check("mas_align_loss", L.mas_align_loss(pm, pl, pz, pr, pw, B, T, S, D, po, gm, gl, gz, ws, n, _stream(stream, dev)))
+    ws, n, keep = _scratch(workspace, lambda: L.mas_align_loss_workspace_bytes(B, T, S, D), mu, stream)
+    _check("mas_align_loss", L.mas_align_loss(pm, pl, pz, pr, pw, B, T, S, D, po, gm, gl, gz, ws, n, _run_on(stream, mu)))
     return loss_out, dmu, dlog_sigma, dz

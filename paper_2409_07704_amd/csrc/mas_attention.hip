@@ -454,7 +454,8 @@ template <class T, int DP> struct Forward {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + 32 * n + acc_row(r, half);
-          s[n][r] = (key >= w.lo) & (key < w.hi) ? s[n][r] : -INFINITY;
+          const bool sees = (key >= w.lo) & (key < w.hi);
+          s[n][r] = sees ? s[n][r] : -INFINITY;
         }
     }
     float top = s[0][0];
@@ -467,7 +468,7 @@ template <class T, int DP> struct Forward {
     // kSlack: p is at most 2^kSlack then, which all types hold, and the sums are
     // seldom rescaled.
     if (__ballot(top > m + kSlack) != 0) {
-      const float to = fmaxf(m, top);
+      const float to = top > m + kSlack ? top : m;  // each row by itself: its result is the same in any company
       const float shrink = __builtin_amdgcn_exp2f(m - (to == -INFINITY ? 0.0f : to));
       l *= shrink;
 #pragma unroll
@@ -498,10 +499,124 @@ template <class T, int DP> __device__ __forceinline__ void load_q(const AttnPara
   for (int c = 0; c < DP / 16; ++c) q[c] = w.used ? load_frag(row, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
 }
 
+// A hidden value must not count whatever it holds, but its p, a 0, does not silence
+// an infinity or a NaN in the product.  So a wave whose sums are not all finite
+// makes them again here: without such elements, and next to that counts which
+// results they do reach, by products with ones for the keys seen: `up` counts
+// infinities and NaN, which become +inf, `down` negative infinities and NaN, which
+// become -inf, both together NaN.  In a cold branch: 32 channels at a time, operands
+// straight from memory, so that it takes fewer registers than the loop before it.
+
+// The rows of one wave over the keys [from, to); with `part` sums, maximum and
+// total go there, at this lane's row.
+template <class T>
+__device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, int b, int hk, int from, int to, float* part) {
+  const int lane = threadIdx.x % 64, half = lane / 32;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const Rows w = rows_of(p, row, b, hk, tq, tk);
+  const ScoreRule rule = score_rule(p);
+  const T* qr = head<T>(p.q, b, w.h) + (int64_t)w.tok * p.q.st;
+  const T* kb = head<T>(p.k, b, hk);
+  const T* vb = head<T>(p.v, b, hk);
+  T* out = head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st;
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+  for (int c0 = 0; c0 < p.D; c0 += 32) {
+    f32x16 o(0.0f), up(0.0f), down(0.0f);
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll 1
+    for (int k0 = from / 32 * 32; k0 < to; k0 += 32) {
+      if (seen(w.lo, w.hi, k0, 32) == Seen::none) continue;
+      const int key = k0 + lane % 32;
+      f32x16 s(0.0f);
+#pragma unroll 1
+      for (int c = 0; c < p.D; c += 16) {
+        const frag<T> kf = key < tk ? load_frag(kb + (int64_t)key * p.k.st, c + 8 * half, p.D, p.vec) : frag<T>(0);
+        const frag<T> qf = w.used ? load_frag(qr, c + 8 * half, p.D, p.vec) : frag<T>(0);
+        s = mma(kf, qf, s);
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int at = k0 + acc_row(r, half);
+        const bool sees = (at >= w.lo) & (at < w.hi);
+        float x = rule.capped ? tanh_of<T>(s[r] * rule.pre) : s[r];
+        x = fmaf(-w.slope, fabsf((float)(w.at - at)), x * rule.mul);
+        s[r] = sees ? x : -INFINITY;
+        top = fmaxf(top, s[r]);
+      }
+      top = max_halves(top);
+      const float high = top > m + kSlack ? top : m, base = high == -INFINITY ? 0.0f : high;
+      const float shrink = __builtin_amdgcn_exp2f(m - base);
+      l *= shrink;
+      o *= shrink;
+      m = high;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] - base);
+        l += s[r];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        frag<T> v, vu, vd, see;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int at = k0 + 16 * h + acc_row(e, half), c = c0 + lane % 32;
+          const T x = at < tk && c < p.D ? vb[(int64_t)at * p.v.st + c] : (T)0.0f;
+          const bool fin = fabsf((float)x) < INFINITY, sees = (at >= w.lo) & (at < w.hi);
+          v[e] = fin ? x : (T)0.0f;
+          vu[e] = fin || (float)x == -INFINITY ? (T)0.0f : (T)1.0f;
+          vd[e] = fin || (float)x == INFINITY ? (T)0.0f : (T)1.0f;
+          see[e] = sees ? (T)1.0f : (T)0.0f;
+        }
+        o = mma(v, acc_frag<T>(s, h), o);
+        up = mma(vu, see, up);
+        down = mma(vd, see, down);
+      }
+    }
+    const float total = add_halves(l), mul = part ? 1.0f : inverse(total);
+    if (!w.in) continue;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int c = c0 + acc_row(r, half);
+      const float mark = (up[r] > 0.0f ? INFINITY : 0.0f) + (down[r] > 0.0f ? -INFINITY : 0.0f);
+      const float x = w.hi > w.lo ? o[r] * mul + mark : 0.0f;
+      if (c >= p.D) continue;
+      if (part)
+        part[c] = x;
+      else
+        out[c] = (T)x;
+    }
+  }
+  if (w.hi <= w.lo) {
+    m = -INFINITY;
+    l = 0.0f;
+  }
+  l = add_halves(l);
+  if (!w.in || lane >= 32) return;
+  if (part) {
+    part[p.D] = m;
+    part[p.D + 1] = l;
+  } else if (p.lse) {
+    p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// Whether a lane's accumulators are finite numbers.
+template <int N> __device__ __forceinline__ bool finite(const f32x16 (&x)[N]) {
+  float t = 0.0f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(x[n][r], 0.0f, t);
+  return t == 0.0f;
+}
+
 // 128 rows a workgroup, 32 a wave; the workgroup shares each tile of keys and
 // values, of which the next is on its way while one is used.
 template <class T, int DP>
-__global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 3 : 2) mas_attention_rows(const AttnParams p) {
   constexpr int KT = kTile<T>, LD = kLd<T, DP>, LDV = kLdCols<T, DP>;
   __shared__ __align__(16) T kt[2][KT * LD];
   __shared__ __align__(16) T vt[2][KT * LDV];
@@ -544,6 +659,8 @@ __global__ void __launch_bounds__(kThreads, 2) mas_attention_rows(const AttnPara
     }
     __syncthreads();
   }
+  if (__ballot(w.hi > w.lo && !finite(f.o)) != 0)
+    return forward_carefully<T>(p, 128 * tile + 32 * wave + lane % 32, b, hk, keys.lo, keys.hi, nullptr);
   if (!w.in) return;
   if (w.hi <= w.lo) f.clear();
   const float l = add_halves(f.l);
@@ -603,7 +720,12 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
     wave_sync();
   }
   if (w.hi <= w.lo) f.clear();
-  __syncthreads();
+  float* part = p.part + (((size_t)at.split * p.pairs + at.pair) * (32 * (size_t)p.tiles) + w.row) * (p.D + 2);
+  // Also the barrier between the tiles and the sums, which share LDS.
+  if (__syncthreads_or(w.hi > w.lo && !finite(f.o))) {
+    if (wave == 0) forward_carefully<T>(p, 32 * tile + lane % 32, b, hk, keys.lo, keys.hi, p.splits > 1 ? part : nullptr);
+    return;
+  }
   if (wave > 0) {
     lds.j.m[wave - 1][lane] = f.m;
     lds.j.l[wave - 1][lane] = f.l;
@@ -632,18 +754,16 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   }
   l = add_halves(l);
   if (p.splits > 1) {
-    const size_t slot = ((size_t)at.split * p.pairs + at.pair) * (32 * (size_t)p.tiles) + w.row;
-    float* o = p.part + slot * (p.D + 2);
     if (lane < 32) {
-      o[p.D] = top;
-      o[p.D + 1] = l;
+      part[p.D] = top;
+      part[p.D + 1] = l;
     }
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int c = 32 * d + acc_row(r, lane / 32);
-        if (c < p.D) o[c] = f.o[d][r];
+        if (c < p.D) part[c] = f.o[d][r];
       }
     return;
   }
@@ -680,13 +800,17 @@ __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams 
     x[1] *= shrink;
     const int n = min(64, p.splits - s0);
     for (int s = 0; s < n; s += 8) {
+      // Lanes past the channels and parts past the end load a neighbour's, for nothing.
+      float v[8][2];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[u][e] = o[(s0 + min(s + u, n - 1)) * stride + min(lane + 64 * e, p.D - 1)];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int i = min(s + u, n - 1);
-        const float w = __shfl(a, i);
+        const float w = s + u < n ? __shfl(a, s + u) : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (lane + 64 * e < p.D && s + u < n) x[e] = fmaf(w, o[(s0 + i) * stride + lane + 64 * e], x[e]);
+        for (int e = 0; e < 2; ++e) x[e] = w != 0.0f ? fmaf(w, v[u][e], x[e]) : x[e];
       }
     }
     top = to;
@@ -761,7 +885,8 @@ template <class T, int DP> struct BackwardQ {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + acc_row(r, half);
-          s[r] = (key >= w.lo) & (key < w.hi) ? s[r] : 0.0f;
+          const bool sees = (key >= w.lo) & (key < w.hi);
+          s[r] = sees ? s[r] : 0.0f;
         }
       }
 #pragma unroll
@@ -1074,7 +1199,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParam
 // exponents.
 template <class T, int DP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_tiles(const AttnParams p) {
-  constexpr int LD = kLd<T, DP>, SUB = 1, RT = 64 * SUB;
+  constexpr int LD = kLd<T, DP>, RT = 64;
   __shared__ __align__(16) T tiles[2][2][RT * LD];
   __shared__ __align__(16) RowTable<RT> table[2];
   __shared__ int range[2 * kMaxWaves];
@@ -1112,8 +1237,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   for (int r0 = first; r0 < rows.hi; r0 += RT, cur ^= 1) {
     const bool more = r0 + RT < rows.hi;
     if (more) fetch(r0 + RT);
-#pragma unroll
-    for (int n = 0; n < SUB; ++n) f.step(tiles[cur][0], tiles[cur][1], LD, table[cur], 64 * n + 32 * by_row, k0, rule, lane);
+    f.step(tiles[cur][0], tiles[cur][1], LD, table[cur], 32 * by_row, k0, rule, lane);
     if (more) put(cur ^ 1);
     __syncthreads();
   }

