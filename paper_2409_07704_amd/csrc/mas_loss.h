@@ -17,7 +17,6 @@ struct LossParams {
   float* part;                      // [B][chunks][2][2][D]: sums of the rows that a chunk's ends cut
   int32_t B, T, S, D;
   int32_t* part_row;                // [B][chunks] the row that begins in the chunk and goes on after it, or -1
-  int32_t past;                     // outputs are too large to stay in the caches until they are used
   int32_t frames, chunks, slabs;    // frames a workgroup, workgroups an item; blocks of channels
 };
 

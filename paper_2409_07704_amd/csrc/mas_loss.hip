@@ -36,13 +36,13 @@ template <int V> __device__ __forceinline__ void load(const float* at, float (&x
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = v[i];
 }
-// past: around the caches.
-template <int V> __device__ __forceinline__ void store(float* at, const float (&x)[V], bool past) {
+// PAST: around the caches.
+template <bool PAST, int V> __device__ __forceinline__ void store(float* at, const float (&x)[V]) {
   typedef float vec __attribute__((ext_vector_type(V)));
   vec v;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = x[i];
-  if (past)
+  if constexpr (PAST)
     __builtin_nontemporal_store(v, reinterpret_cast<vec*>(at));
   else
     *reinterpret_cast<vec*>(at) = v;
@@ -54,7 +54,7 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-template <int V, int GL>
+template <int V, int GL, bool PAST>
 __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) {
   constexpr int kGroups = kThreads / GL, kCols = GL * V;
   constexpr int kMaxFrames = kGroups * 16;
@@ -100,12 +100,12 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
         if (p.dmu) {
 #pragma unroll
           for (int i = 0; i < V; ++i) x[i] = -weight * am[i];
-          store(p.dmu + at, x, p.past);
+          store<PAST>(p.dmu + at, x);
         }
         if (p.dlog_sigma) {
 #pragma unroll
           for (int i = 0; i < V; ++i) x[i] = weight * al[i];
-          store(p.dlog_sigma + at, x, p.past);
+          store<PAST>(p.dlog_sigma + at, x);
         }
       }
     } else if (slot < 2 * group + 2) {  // two at most: the first and the last row of the run
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
           g[i] = weight * y;
         }
       }
-      if (dz && in) store(dz + (size_t)(k + u) * p.D, g, p.past);
+      if (dz && in) store<PAST>(dz + (size_t)(k + u) * p.D, g);
     }
   }
   flush();
@@ -178,8 +178,8 @@ __global__ void __launch_bounds__(kThreads) mas_loss_kernel(const LossParams p) 
       float zero[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) zero[v] = 0.0f;
-      if (p.dmu) store(p.dmu + at, zero, p.past);
-      if (p.dlog_sigma) store(p.dlog_sigma + at, zero, p.past);
+      if (p.dmu) store<PAST>(p.dmu + at, zero);
+      if (p.dlog_sigma) store<PAST>(p.dlog_sigma + at, zero);
     }
   if (tid >= kCols || slab * kCols + tid >= p.D) return;
   // Rows cut by the ends of runs, a channel a thread.
@@ -263,7 +263,11 @@ size_t bytes_of(const LossParams& p) {
 }
 
 template <int V, int GL> hipError_t launch(const LossParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL((mas_loss_kernel<V, GL>), dim3((uint32_t)p.B * p.chunks * p.slabs), dim3(kThreads), 0, stream, p);
+  const dim3 grid((uint32_t)p.B * p.chunks * p.slabs);
+  if (4.0 * p.B * ((double)p.S + 2.0 * p.T) * p.D > kPastBytes)
+    hipLaunchKernelGGL((mas_loss_kernel<V, GL, true>), grid, dim3(kThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL((mas_loss_kernel<V, GL, false>), grid, dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -283,7 +287,6 @@ size_t loss_workspace_bytes(int32_t B, int32_t T, int32_t S, int32_t D) {
 
 hipError_t launch_loss(LossParams p, bool vec, void* workspace, hipStream_t stream) {
   plan(p, vec ? 4 : 1);
-  p.past = 4.0 * p.B * ((double)p.S + 2.0 * p.T) * p.D > kPastBytes;
   p.part = static_cast<float*>(workspace);
   p.part_loss = p.part + (size_t)p.B * p.chunks * 4 * p.D;
   p.part_row = reinterpret_cast<int32_t*>(p.part_loss + (size_t)p.B * p.chunks * p.slabs);

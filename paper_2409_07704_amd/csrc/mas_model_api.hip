@@ -121,7 +121,6 @@ QkParams params(const mas_qk_desc& d, std::initializer_list<const mas_heads*> al
   p.P = d.P > 0 ? d.P : 1;
   p.interleaved = d.interleaved != 0;
   p.eps = d.eps;
-  p.past = (double)d.B * d.T * (d.Hq + d.Hk) * d.D * elem_bytes(d.dtype) > kPastBytes;
   p.align = 16;
   for (const mas_heads* h : all)
     if (given(h)) {

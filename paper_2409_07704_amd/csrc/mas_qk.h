@@ -24,7 +24,6 @@ struct QkParams {
   float *dwq, *dwk;         // [D] or null
   int32_t B, T, Hq, Hk, D, R, P, interleaved;
   int32_t align;            // every head starts on a multiple of this many elements (a power of two)
-  int32_t past;             // outputs are too large to stay in the caches until they are used
   float eps;
 };
 

@@ -35,13 +35,13 @@ template <class T, int V> __device__ __forceinline__ void load(const T* at, floa
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = (float)v[i];
 }
-// past: around the caches.
-template <class T, int V> __device__ __forceinline__ void store(T* at, const float (&x)[V], bool past) {
+// PAST: around the caches.
+template <bool PAST, class T, int V> __device__ __forceinline__ void store(T* at, const float (&x)[V]) {
   typename Pack<T, V>::type v;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = (T)x[i];
   auto* to = reinterpret_cast<typename Pack<T, V>::type*>(at);
-  if (past)
+  if constexpr (PAST)
     __builtin_nontemporal_store(v, to);
   else
     *to = v;
@@ -123,7 +123,7 @@ template <int V> __device__ __forceinline__ void weights(const float* w, int c0,
 }
 
 // U: heads a group has in flight.
-template <class T, int V, int GL, int U>
+template <class T, int V, int GL, int U, bool PAST>
 __global__ void __launch_bounds__(kThreads) mas_qk_kernel(const QkParams p, int parts) {
   const size_t n = ((size_t)blockIdx.x * kThreads + threadIdx.x) / GL;
   if (n >= (size_t)p.B * p.T * parts) return;  // whole groups
@@ -154,12 +154,12 @@ __global__ void __launch_bounds__(kThreads) mas_qk_kernel(const QkParams p, int 
 #pragma unroll
       for (int i = 0; i < V; ++i) x[u][i] = s.used ? x[u][i] * (r * (h < p.Hq ? wq[i] : wk[i])) : 0.0f;
       turn.apply(x[u], 1.0f);
-      if (in && h < s.heads) store(head<T>(p, p.qo, p.ko, s, h) + c0, x[u], p.past);
+      if (in && h < s.heads) store<PAST>(head<T>(p, p.qo, p.ko, s, h) + c0, x[u]);
     }
   }
 }
 
-template <class T, int V, int GL, int U>
+template <class T, int V, int GL, int U, bool PAST>
 __global__ void __launch_bounds__(kThreads) mas_qk_backward_kernel(const QkParams p, int parts) {
   constexpr int kGroups = kThreads / GL;
   __shared__ float sums[kGroups][GL * V];
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) mas_qk_backward_kernel(const QkParam
         const float mean = group_sum<GL>(dot) / (float)p.D;
 #pragma unroll
         for (int i = 0; i < V; ++i) x[u][i] = counts ? r * fmaf(-x[u][i], mean, g[u][i]) : 0.0f;
-        if (in && h < s.heads) store(head<T>(p, p.dq, p.dk, s, h) + c0, x[u], p.past);
+        if (in && h < s.heads) store<PAST>(head<T>(p, p.dq, p.dk, s, h) + c0, x[u]);
       }
     }
   }
@@ -370,20 +370,21 @@ int parts_of(const QkParams& p) {
   return parts < heads ? parts : heads;
 }
 
-template <class T, int V, int GL, int U> hipError_t launch_u(const QkParams& p, int parts, bool back, hipStream_t stream) {
+template <class T, int V, int GL, int U, bool PAST> hipError_t launch_u(const QkParams& p, int parts, bool back, hipStream_t stream) {
   if (back) {
-    hipLaunchKernelGGL((mas_qk_backward_kernel<T, V, GL, U>), dim3(qk_backward_blocks(p.B, p.T, p.Hq + p.Hk)), dim3(kThreads), 0, stream, p, parts);
+    hipLaunchKernelGGL((mas_qk_backward_kernel<T, V, GL, U, PAST>), dim3(qk_backward_blocks(p.B, p.T, p.Hq + p.Hk)), dim3(kThreads), 0, stream, p, parts);
   } else {
     const uint64_t groups = (uint64_t)p.B * p.T * parts;
-    hipLaunchKernelGGL((mas_qk_kernel<T, V, GL, U>), dim3((uint32_t)((groups * GL + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p, parts);
+    hipLaunchKernelGGL((mas_qk_kernel<T, V, GL, U, PAST>), dim3((uint32_t)((groups * GL + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream, p, parts);
   }
   return hipGetLastError();
 }
 
 template <class T, int V, int GL> hipError_t launch(const QkParams& p, bool back, hipStream_t stream) {
   const int parts = parts_of(p);
-  const bool many = (p.Hq + p.Hk) / parts >= kInFlight;
-  return many ? launch_u<T, V, GL, kInFlight>(p, parts, back, stream) : launch_u<T, V, GL, 1>(p, parts, back, stream);
+  if ((p.Hq + p.Hk) / parts < kInFlight) return launch_u<T, V, GL, 1, false>(p, parts, back, stream);
+  const bool past = (double)p.B * p.T * (p.Hq + p.Hk) * p.D * sizeof(T) > kPastBytes;
+  return past ? launch_u<T, V, GL, kInFlight, true>(p, parts, back, stream) : launch_u<T, V, GL, kInFlight, false>(p, parts, back, stream);
 }
 
 template <class T> hipError_t launch_any(const QkParams& p, bool back, hipStream_t stream) {
