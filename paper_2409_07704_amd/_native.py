@@ -376,6 +376,8 @@ def _empty(shape, dtype, device, stream):
 def _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix):
     if not isinstance(q, torch.Tensor) or not isinstance(k, torch.Tensor) or q.dim() != 4 or k.dim() != 4:
         raise ValueError("q must be [B, Tq, Hq, D] and k [B, Tk, Hk, D]")
+    if not q.is_cuda:
+        raise TypeError("q must be a device (cuda/hip) tensor")
     B, Tq, Hq, D = q.shape
     _, Tk, Hk, _ = k.shape
     N = 1
@@ -445,6 +447,8 @@ def mas_attention_backward(dout, q, k, v, out, lse, t_q=None, t_k=None, causal=F
 def _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved):
     if not isinstance(q, torch.Tensor) or q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q must be [B, T, Hq, D] and k [B, T, Hk, D] or None")
+    if not q.is_cuda:
+        raise TypeError("q must be a device (cuda/hip) tensor")
     B, T, Hq, D = q.shape
     Hk = 0 if k is None else k.shape[2]
     if (cos is None) != (sin is None) or (cos is not None and cos.dim() != 2):
