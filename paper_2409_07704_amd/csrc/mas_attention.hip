@@ -118,6 +118,7 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.
 struct Interval {
   int lo, hi;
 };
+constexpr int kFewDocs = 12;
 
 // Keys that the query at `place` of item b sees; tk is the item's key length.
 __device__ __forceinline__ Interval interval(const AttnParams& p, int b, int place, int tk) {
@@ -125,20 +126,39 @@ __device__ __forceinline__ Interval interval(const AttnParams& p, int b, int pla
   int pre = 0;
   if (p.doc_start) {
     const int32_t* t = p.doc_start + (size_t)b * (p.N + 1);
-    int first = 0, n = p.N + 1;  // starts up to `place`: the first n of them are candidates
-    while (n > 0) {
-      const int step = n / 2;
-      if (t[first + step] <= place) {
-        first += step + 1;
-        n -= step + 1;
-      } else {
-        n = step;
+    int first = 0;  // starts up to `place`
+    if (p.N <= kFewDocs) {
+      // Few documents: all starts at once, one wait instead of one a step.
+      int from = 0, to = 0;
+#pragma unroll
+      for (int n = 0; n <= kFewDocs; ++n) {
+        const int at = t[min(n, p.N)];
+        const int len = p.prefix ? p.prefix[(size_t)b * p.N + min(n, p.N - 1)] : 0;
+        const bool before = n <= p.N && at <= place;
+        to = before || first < n ? to : at;
+        from = before ? at : from;
+        pre = before ? len : pre;
+        first = before ? n + 1 : first;
       }
+      if (first == 0 || first > p.N) return {0, 0};
+      lo = max(from, 0);
+      hi = min(to, tk);
+    } else {
+      int n = p.N + 1;
+      while (n > 0) {
+        const int step = n / 2;
+        if (t[first + step] <= place) {
+          first += step + 1;
+          n -= step + 1;
+        } else {
+          n = step;
+        }
+      }
+      if (first == 0 || first > p.N) return {0, 0};
+      lo = max(t[first - 1], 0);
+      hi = min(t[first], tk);
+      if (p.prefix) pre = p.prefix[(size_t)b * p.N + first - 1];
     }
-    if (first == 0 || first > p.N) return {0, 0};
-    lo = max(t[first - 1], 0);
-    hi = min(t[first], tk);
-    if (p.prefix) pre = p.prefix[(size_t)b * p.N + first - 1];
   } else if (p.prefix) {
     pre = p.prefix[b];
   }
@@ -1247,6 +1267,148 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   if (by_row == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
 }
 
+// The same for more than 64 channels, whose two sums do not fit the registers of
+// one wave next to another's: two waves share a block of 32 keys by 32 rows.  One
+// makes the scores, p and dv; the other, a tile later, takes p (1 - tanh^2) from
+// LDS, where it lies lane by lane, makes ds and dk.  So each holds one operand and
+// one sum, and while one takes exponents the other, on the same SIMD, multiplies.
+// Eight waves: both kinds, two blocks of keys, two of rows; three tiles of 64
+// rows: in use by the first kind, by the second, on its way.
+template <class T, int DP>
+__global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const AttnParams p) {
+  constexpr int LD = kLd<T, DP>, RT = 64;
+  __shared__ __align__(16) T tiles[3][2][RT * LD];
+  __shared__ __align__(16) f32x4 probs[2][4][4][64];
+  __shared__ __align__(16) RowTable<RT> table[3];
+  __shared__ int range[2 * kMaxWaves];
+  static_assert(sizeof(tiles) >= 4 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+  const Place at = place_of(p);
+  if (at.idle) return;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int tid = threadIdx.x, lane = tid % 64, half = lane / 32, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int by_key = wave % 2, by_row = wave / 2 % 2, block = wave % 4;
+  const bool scores = wave < 4;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int kb0 = 64 * at.tile, k0 = kb0 + 32 * by_key, key = k0 + lane % 32;
+  // The block's keys, or its values.
+  frag<T> own[DP / 16];
+  {
+    const HeadView& v = scores ? p.k : p.v;
+    const T* row = head<T>(v, b, hk) + (int64_t)key * v.st;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) own[c] = key < tk ? load_frag(row, 16 * c + 8 * half, p.D, p.vec) : frag<T>(0);
+  }
+  const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
+  const ScoreRule rule = score_rule(p);
+  // The first kind brings the queries, the second the gradients.
+  const HeadView brings = scores ? p.q : p.dout;
+  Stage<T, DP, RT, kThreads, true> st(p, brings, b, hk, tq * p.G, tid % kThreads);
+  RowInfo info;
+  f32x16 sum[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) sum[d] = f32x16(0.0f);
+  const int first = rows.lo / 32 * 32, n = (rows.hi - first + RT - 1) / RT;
+  const auto fetch = [&](int t) {
+    info.load(p, b, hk, first + RT * t + tid % RT);
+    st.load(first + RT * t);
+  };
+  const auto put = [&](int to) {
+    st.store(tiles[to][scores ? 0 : 1], LD);
+    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi);
+  };
+  if (n > 0) {
+    fetch(0);
+    put(0);
+  }
+  __syncthreads();
+  int cur = 0;  // the tile of the first kind, modulo 3
+  for (int t = 0; t <= n && n > 0; ++t) {
+    const int next = cur == 2 ? 0 : cur + 1, last = cur == 0 ? 2 : cur - 1;
+    if (t + 1 < n) fetch(t + 1);
+    const int mine = scores ? cur : last;
+    const RowTable<RT>& tab = table[mine];
+    const int i0 = 32 * by_row, i = i0 + 4 * half;
+    const bool turn = scores ? t < n : t > 0;
+    const int lo = tab.lo[i0 + lane % 32], hi = tab.hi[i0 + lane % 32];
+    if (turn && __ballot(lo < k0 + 32 && hi > k0) != 0) {
+      f32x4(&pr)[4][64] = probs[(scores ? t : t - 1) & 1][block];
+      const T* rt = tiles[mine][scores ? 0 : 1] + i0 * LD;
+      f32x16 s(0.0f);
+      {
+        frag<T> x[DP / 16];
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) x[c] = rows_frag(rt, LD, 16 * c, lane);
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) s = mma(x[c], own[c], s);
+      }
+      if (scores) {
+        f32x16 bend(1.0f);
+        if (rule.capped) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[r] = tanh_of<T>(s[r] * rule.pre);
+            bend[r] = fmaf(-s[r], s[r], 1.0f);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 lse = four_at<f32x4>(&tab.lse[i + 2 * r]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, -lse[e]);
+        }
+        if (rule.sloped) {
+          const float place = (float)key;
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const f32x4 slope = four_at<f32x4>(&tab.slope[i + 2 * r]), where = four_at<f32x4>(&tab.at[i + 2 * r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[r + e] = fmaf(-slope[e], fabsf(where[e] - place), s[r + e]);
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
+        // Rows that see nothing have no statistics: they are masked, not taken for full.
+        if (__ballot(lo <= k0 && hi >= k0 + 32) != ~0ull) {
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const i32x4 from = four_at<i32x4>(&tab.lo[i + 2 * r]), to = four_at<i32x4>(&tab.hi[i + 2 * r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool sees = (key >= from[e]) & (key < to[e]);
+              s[r + e] = sees ? s[r + e] : 0.0f;
+            }
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) pr[r / 4][lane] = f32x4{s[r] * bend[r], s[r + 1] * bend[r + 1], s[r + 2] * bend[r + 2], s[r + 3] * bend[r + 3]};
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 delta = four_at<f32x4>(&tab.delta[i + 2 * r]), x = pr[r / 4][lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r + e] = x[e] != 0.0f ? x[e] * (s[r + e] - delta[e]) : 0.0f;
+        }
+      }
+      const T* ct = tiles[mine][scores ? 1 : 0] + i0 * LD;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const frag<T> f = acc_frag<T>(s, h);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) sum[d] = mma(cols_frag(ct, LD, h, 32 * d, lane), f, sum[d]);
+      }
+    }
+    if (t + 1 < n) put(next);
+    __syncthreads();
+    cur = next;
+  }
+  add_waves<2>(sum, reinterpret_cast<float*>(tiles) + (wave / 4 * 2 + by_key) * ((DP / 32) * 16 * 64), by_row, lane);
+  if (by_row != 0 || key >= p.Tk) return;
+  if (scores)
+    store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, sum, 1.0f, half, p.D, p.vec);
+  else
+    store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, sum, p.scale, half, p.D, p.vec);
+}
+
 // Workgroups, and how place_of deals them out: over the dies if the last, partly
 // used round of eight pairs is a small part.
 uint32_t grid_of(AttnParams& p) {
@@ -1286,7 +1448,10 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
     p.tiles = (p.Tk + 63) / 64;
     if ((int64_t)p.tiles * p.pairs >= 256) {
       grid = grid_of(p);
-      hipLaunchKernelGGL((mas_attention_dkv_tiles<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+      if constexpr (DP > 64)
+        hipLaunchKernelGGL((mas_attention_dkv_pairs<T, DP>), dim3(grid), dim3(2 * kThreads), 0, stream, p);
+      else
+        hipLaunchKernelGGL((mas_attention_dkv_tiles<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
       return hipGetLastError();
     }
   }
