@@ -221,6 +221,21 @@ template <class T> __device__ __forceinline__ frag<T> load_frag(const T* row, in
   return u.f;
 }
 
+// A tile in LDS.  16-bit types: rows of DP elements whose 16-byte pieces are dealt out
+// anew in every row, piece c of row r at c ^ turned(r).  The LDS gives 256 bytes a
+// cycle, 64 banks: 16 lanes of a read of rows, a piece of 16 rows each, or 32 lanes of
+// a transposing read, 64 bytes of 4 rows each.  So of 16 rows each has another turn
+// (as far as rows share banks), and of 4 neighbours each another one in units of 64
+// bytes.  (Rows 16 bytes longer instead suit only the reads of rows: the transposing
+// ones took four times as long.)  fp32: rows 16 bytes longer, or not where only columns
+// are read.
+template <class T, int DP> constexpr int kLd = DP + (sizeof(T) == 4 ? 4 : 0);
+template <class T, int DP> constexpr int kLdCols = DP;
+template <class T> __device__ __forceinline__ int turned(int row, int ld) {
+  if (sizeof(T) == 4) return 0;
+  return row / 4 % 4 ^ (ld % 128 == 0 ? row % 4 * 4 : ld % 64 == 0 ? row / 2 % 2 * 4 : 0);
+}
+
 // Tiles of ROWS rows of DP channels on their way from memory to LDS, spread over
 // TEAM threads in 16-byte pieces: rows k of one head, st apart, or (BY_ROWS) rows of
 // the group's row axis.  Where a tile is inside the tensor, rows are whole aligned
@@ -236,8 +251,10 @@ template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
   int tid, limit; // zeros from row `limit` on
   bool fast, whole;
   int at;
+  // A head's pieces of one thread lie evenly apart where threads are whole rows.
+  static constexpr bool kEven = !BY_ROWS && TEAM % CPR == 0;
   u32x4 r[N];
-  uint32_t off[N];
+  uint32_t off[kEven ? 1 : N];
   __device__ __forceinline__ int row(int n) const { return (tid + n * TEAM) / CPR; }
   __device__ __forceinline__ int col(int n) const { return (tid + n * TEAM) % CPR * E; }
   __device__ __forceinline__ Stage(const AttnParams& p, const HeadView& v, int b, int hk, int limit, int tid)
@@ -245,7 +262,7 @@ template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
     const int most = (1 << 29) / (ROWS * (int)sizeof(T));
     fast = p.vec && v.st < most && (!BY_ROWS || (32 % p.G == 0 && v.sh < most));
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
+    for (int n = 0; n < (kEven ? 1 : N); ++n) {
       const int i = row(n), c = col(n) < p.D ? col(n) : 0;
       const int o = BY_ROWS ? (i >> p.g_shift) * (int)v.st + (i & (p.G - 1)) * (int)v.sh : i * (int)v.st;
       off[n] = (uint32_t)(o + c) * (uint32_t)sizeof(T);
@@ -258,7 +275,8 @@ template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
     if (!whole) return;
     const char* tile = reinterpret_cast<const char*>(base + (int64_t)(BY_ROWS ? k0 >> p.g_shift : k0) * v.st);
 #pragma unroll
-    for (int n = 0; n < N; ++n) r[n] = *reinterpret_cast<const u32x4*>(tile + off[n]);
+    for (int n = 0; n < N; ++n)
+      r[n] = *reinterpret_cast<const u32x4*>(kEven ? tile + (int64_t)(n * (TEAM / CPR)) * v.st * (int)sizeof(T) + off[0] : tile + off[n]);
   }
   __device__ __forceinline__ u32x4 slow(int i, int c) const {
     if (i >= limit) return u32x4(0);
@@ -266,24 +284,20 @@ template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
     const int tok = token_of(p, i);
     return load16(base + (int64_t)(i - tok * p.G) * v.sh + (int64_t)tok * v.st, c, p.D, p.vec);
   }
+  __device__ __forceinline__ u32x4* place(T* lds, int ld, int n) const {
+    return reinterpret_cast<u32x4*>(lds + row(n) * ld + ((col(n) / E) ^ turned<T>(row(n), ld)) * E);
+  }
   __device__ __forceinline__ void store(T* lds, int ld) const {
     if (whole) {
       const bool all = p.D == DP;
 #pragma unroll
-      for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n) * ld + col(n)) = all || col(n) < p.D ? r[n] : u32x4(0);
+      for (int n = 0; n < N; ++n) *place(lds, ld, n) = all || col(n) < p.D ? r[n] : u32x4(0);
     } else {
 #pragma unroll 1
-      for (int n = 0; n < N; ++n) *reinterpret_cast<u32x4*>(lds + row(n) * ld + col(n)) = slow(at + row(n), col(n));
+      for (int n = 0; n < N; ++n) *place(lds, ld, n) = slow(at + row(n), col(n));
     }
   }
 };
-
-// Leading dimension of a tile in LDS: 16 bytes more than the row, so that the 32
-// rows of an operand read start on different banks.
-template <class T, int DP> constexpr int kLd = DP + 16 / (int)sizeof(T);
-// And of a tile whose columns are read: the four rows of a transposing read on
-// different banks.
-template <class T, int DP> constexpr int kLdCols = sizeof(T) == 4 ? DP : DP % 64 == 0 ? DP + 16 : DP + 48;
 
 // Operand from rows of a tile: lane l holds row l % 32, channels c + 8 (l / 32) ...
 template <class T> __device__ __forceinline__ frag<T> rows_frag(const T* tile, int ld, int c, int lane) {
@@ -291,9 +305,11 @@ template <class T> __device__ __forceinline__ frag<T> rows_frag(const T* tile, i
     u32x4 v[sizeof(frag<T>) / 16];
     frag<T> f;
   } u;
-  const u32x4* at = reinterpret_cast<const u32x4*>(tile + (lane % 32) * ld + c + 8 * (lane / 32));
+  constexpr int E = 16 / sizeof(T);
+  const int row = lane % 32, piece = c / E + 8 / E * (lane / 32);
 #pragma unroll
-  for (int i = 0; i < (int)(sizeof(frag<T>) / 16); ++i) u.v[i] = at[i];
+  for (int i = 0; i < (int)(sizeof(frag<T>) / 16); ++i)
+    u.v[i] = *reinterpret_cast<const u32x4*>(tile + row * ld + ((piece + i) ^ turned<T>(row, ld)) * E);
   return u.f;
 }
 
@@ -311,13 +327,14 @@ template <class T> __device__ __forceinline__ frag<T> cols_frag(const T* tile, i
     // get it transposed: a channel each, of the four rows.
     typedef __attribute__((address_space(3))) s16x4* lds_ptr;
     const int j = lane % 16;
-    const T* at = tile + (16 * m + 4 * h + j / 4) * ld + c + 16 * (lane / 16 % 2) + 4 * (j % 4);
+    const int row = 4 * h + j / 4, piece = c / 8 + 2 * (lane / 16 % 2) + j % 4 / 2;
+    const T* at = tile + (16 * m + row) * ld + 4 * (j % 2);
     union {
       s16x4 q[2];
       frag<T> f;
     } u;
-    u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
-    u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * ld));
+    u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + (piece ^ turned<T>(row, ld)) * 8));
+    u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * ld + (piece ^ turned<T>(row + 8, ld)) * 8));
     return u.f;
   }
 }
@@ -922,7 +939,7 @@ template <class T, int DP> struct BackwardQ {
 // FEW: 32 rows a workgroup, its waves take the blocks of keys in turn; else 128
 // rows a workgroup with shared tiles, as in the forward pass.
 template <class T, int DP, bool FEW>
-__global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : 2) mas_attention_dq(const AttnParams p) {
+__global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2) mas_attention_dq(const AttnParams p) {
   constexpr int KT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
   __shared__ __align__(16) T kt[SETS][KT * LD];
   __shared__ __align__(16) T vt[SETS][KT * LD];
@@ -1386,7 +1403,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
         for (int r = 0; r < 16; r += 4) {
           const f32x4 delta = four_at<f32x4>(&tab.delta[i + 2 * r]), x = pr[r / 4][lane];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[r + e] = x[e] != 0.0f ? x[e] * (s[r + e] - delta[e]) : 0.0f;
+          for (int e = 0; e < 4; ++e) s[r + e] = x[e] * (s[r + e] - delta[e]);
         }
       }
       const T* ct = tiles[mine][scores ? 1 : 0] + i0 * LD;
