@@ -40,7 +40,7 @@ struct AttnPlan {
   bool small;  // workgroups of 32 rows whose four waves take turns at the keys
   int32_t tiles, splits, span;
 };
-AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk);
+AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32);
 size_t attention_part_bytes(const AttnPlan& plan, int32_t pairs, int32_t D);
 
 hipError_t launch_attention(AttnParams p, int dtype, const AttnPlan& plan, hipStream_t stream);

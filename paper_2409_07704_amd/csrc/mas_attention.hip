@@ -1449,7 +1449,8 @@ template <class T, int DP> hipError_t forward(AttnParams p, const AttnPlan& plan
 
 template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream) {
   p.splits = 1;
-  // 128 rows a workgroup where those fill the 256 compute units, else 32.
+  // 128 rows a workgroup where those fill the 256 compute units, else 32 (1024 keys of
+  // 64 channels, bf16, with dk, dv: 128 workgroups 53.4 / 44.4 us, 256 60.5 / 62.8).
   p.tiles = (p.rows + 127) / 128;
   const bool few_rows = (int64_t)p.tiles * p.pairs < 256;
   if (few_rows) p.tiles = (p.rows + 31) / 32;
@@ -1461,7 +1462,8 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 2) {
-    // 64 keys a workgroup where those fill the compute units.
+    // 64 keys a workgroup where those fill the compute units, else 32 (512 keys of 64
+    // channels, bf16, with dq: 128 workgroups of 64 keys 28.3 / 25.4 us, 256 30.9 / 38.4).
     p.tiles = (p.Tk + 63) / 64;
     if ((int64_t)p.tiles * p.pairs >= 256) {
       grid = grid_of(p);
@@ -1487,19 +1489,31 @@ template <class T, class F> hipError_t by_width(int D, F&& f) {
 
 }  // namespace
 
-AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk) {
+AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32) {
   AttnPlan a;
   a.splits = 1;
   a.span = Tk;
   a.tiles = (rows + 127) / 128;
-  a.small = rows <= 32 || (int64_t)a.tiles * pairs < 256;
+  // Workgroups of 128 rows where they fill the compute units (256; from half of them
+  // on with more than 64 channels in 16 bits, where those of 32 rows fit a unit only
+  // once), else of 32 rows whose waves share the keys.  Measured, 128 / 32 rows, causal,
+  // 512 keys of 64 channels, bf16: 128 workgroups 16.0 / 13.0 us, 256 16.3 / 21.6; 1024
+  // keys 24.9 / 17.9 and 25.2 / 26.6; 128 channels, 512 keys, 128 workgroups 23.1 / 29.2,
+  // 1024 keys, 32 workgroups 35.7 / 23.1; fp32, 512 keys of 64 channels, 128 workgroups
+  // 45.2 / 29.2, 256 49.4 / 49.1.  Up to 32 rows always the latter (64 caches of 4096
+  // keys, 4 heads: 128 / 43; 512 of 1024 keys 25.7 / 26.1; 2048 of 256 keys 32.3 / 37.6).
+  a.small = rows <= 32 || (int64_t)a.tiles * pairs < (fp32 || D <= 64 ? 256 : 128);
   if (!a.small) return a;
   a.tiles = (rows + 31) / 32;
-  // Parts of at least 128 keys, a block for every wave, until two workgroups a
-  // compute unit are there.
+  // The keys are split until two workgroups a compute unit are there, into parts of at
+  // least 512, four blocks a wave; steps over more than 1024 keys into parts of 128.
+  // Measured with 128 / 512 at least: a step over 2048 keys 16.3 / 20.7 us, over 1024
+  // keys 15.0 / 15.9; 64 workgroups of 32 rows by 512 keys 13.6 / 10.9 (the second
+  // kernel, which joins the parts, takes 5).
+  const int least = rows <= 32 && Tk > 1024 ? 128 : 512;
   const int64_t groups = (int64_t)a.tiles * pairs;
   int64_t want = (512 + groups - 1) / groups;
-  const int64_t most = (Tk + 127) / 128;
+  const int64_t most = (Tk + least - 1) / least;
   if (want > most) want = most;
   a.span = (int32_t)(((Tk + want - 1) / want + 127) / 128 * 128);
   a.splits = (Tk + a.span - 1) / a.span;

@@ -253,7 +253,9 @@ int lanes_of(int D, int V) {
 void plan(LossParams& p, int V) {
   const int lanes = lanes_of(p.D, V), groups = kThreads / lanes;
   p.slabs = (p.D + lanes * V - 1) / (lanes * V);
-  // Runs of 16 frames; of 4 where those would leave compute units without work.
+  // Runs of 16 frames; of 4 where those would leave compute units without work
+  // (measured, 16 / 4: 16 x 512 frames of 80 channels 16.3 / 13.7 us, 32 x 1024 of 192
+  // 20.0 / 20.0, 64 x 2048 of 192 49.3 / 57.1).
   const int64_t blocks = (int64_t)p.B * p.slabs * ((p.S + 16 * groups - 1) / (16 * groups));
   p.frames = groups * (blocks >= 1024 ? 16 : 4);
   p.chunks = (p.S + p.frames - 1) / p.frames;

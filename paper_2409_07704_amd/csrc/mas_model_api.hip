@@ -140,7 +140,7 @@ extern "C" {
 size_t mas_attention_workspace_bytes(const mas_attention_desc* desc, int32_t backward) {
   if (check_desc(desc) != MAS_OK) return 0;
   const int32_t pairs = desc->B * desc->Hk;
-  const AttnPlan plan = attention_plan(pairs, desc->Tq * (desc->Hq / desc->Hk), desc->Tk);
+  const AttnPlan plan = attention_plan(pairs, desc->Tq * (desc->Hq / desc->Hk), desc->Tk, desc->D, desc->dtype == MAS_F32);
   size_t n = attention_part_bytes(plan, pairs, desc->D);
   if (backward && stat_bytes(*desc) > n) n = stat_bytes(*desc);
   return round_up(n > 0 ? n : 1);
@@ -155,7 +155,7 @@ mas_status mas_attention(const mas_attention_desc* desc, const mas_heads* q, con
   for (const mas_heads* h : {q, k, v, out})
     if (!elements_ok(*h, elem_bytes(desc->dtype))) return MAS_ERR_BAD_VALUE;
   AttnParams p = params(*desc);
-  const AttnPlan plan = attention_plan(p.pairs, p.rows, p.Tk);
+  const AttnPlan plan = attention_plan(p.pairs, p.rows, p.Tk, p.D, desc->dtype == MAS_F32);
   if (!workspace_ok(workspace, workspace_bytes, attention_part_bytes(plan, p.pairs, p.D))) return MAS_ERR_WORKSPACE;
   p.q = view(q);
   p.k = view(k);
