@@ -38,6 +38,7 @@ struct AttnParams {
 // How the forward pass is laid out on the chip.
 struct AttnPlan {
   bool small;  // workgroups of 32 rows whose four waves take turns at the keys
+  int32_t waves;  // else: of 32 rows each in a workgroup
   int32_t tiles, splits, span;
 };
 AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32);

@@ -671,10 +671,10 @@ template <int N> __device__ __forceinline__ bool finite(const f32x16 (&x)[N]) {
   return t == 0.0f;
 }
 
-// 128 rows a workgroup, 32 a wave; the workgroup shares each tile of keys and
+// W waves a workgroup, 32 rows a wave; the workgroup shares each tile of keys and
 // values, of which the next is on its way while one is used.
-template <class T, int DP>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 3 : 2) mas_attention_rows(const AttnParams p) {
+template <class T, int DP, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 3 : 2) mas_attention_rows(const AttnParams p) {
   constexpr int KT = kTile<T>, LD = kLd<T, DP>, LDV = kLdCols<T, DP>;
   __shared__ __align__(16) T kt[2][KT * LD];
   __shared__ __align__(16) T vt[2][KT * LDV];
@@ -686,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 3 : 2) 
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   // The last rows see most where the mask is causal: they start first.
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
-  const Rows w = rows_of(p, 128 * tile + 32 * wave + lane % 32, b, hk, tq, tk);
+  const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
   const ScoreRule rule = score_rule(p);
 
@@ -694,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 3 : 2) 
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
   f.start();
 
-  Stage<T, DP, KT, kThreads, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
+  Stage<T, DP, KT, 64 * W, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
   const int first = keys.lo / KT * KT;
   if (first < keys.hi) {
     ks.load(first);
@@ -718,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 3 : 2) 
     __syncthreads();
   }
   if (__ballot(w.hi > w.lo && !finite(f.o)) != 0)
-    return forward_carefully<T>(p, 128 * tile + 32 * wave + lane % 32, b, hk, keys.lo, keys.hi, nullptr);
+    return forward_carefully<T>(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, keys.lo, keys.hi, nullptr);
   if (!w.in) return;
   if (w.hi <= w.lo) f.clear();
   const float l = add_halves(f.l);
@@ -957,10 +957,10 @@ template <class T, int DP> struct BackwardQ {
   }
 };
 
-// FEW: 32 rows a workgroup, its waves take the blocks of keys in turn; else 128
-// rows a workgroup with shared tiles, as in the forward pass.
-template <class T, int DP, bool FEW>
-__global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2) mas_attention_dq(const AttnParams p) {
+// FEW: 32 rows a workgroup, its four waves take the blocks of keys in turn; else W
+// waves of 32 rows with shared tiles, as in the forward pass.
+template <class T, int DP, bool FEW, int W>
+__global__ void __launch_bounds__(64 * W, FEW || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2) mas_attention_dq(const AttnParams p) {
   constexpr int KT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
   __shared__ __align__(16) T kt[SETS][KT * LD];
   __shared__ __align__(16) T vt[SETS][KT * LD];
@@ -972,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : DP <= 64
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
-  const Rows w = rows_of(p, FEW ? 32 * tile + lane % 32 : 128 * tile + 32 * wave + lane % 32, b, hk, tq, tk);
+  const Rows w = rows_of(p, FEW ? 32 * tile + lane % 32 : 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
   const ScoreRule rule = score_rule(p);
 
@@ -1020,7 +1020,7 @@ __global__ void __launch_bounds__(kThreads, FEW || sizeof(T) == 4 ? 1 : DP <= 64
     add_waves<kWaves>(f.dq, reinterpret_cast<float*>(kt), wave, lane);
     if (wave > 0) return;
   } else {
-    Stage<T, DP, KT, kThreads, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
+    Stage<T, DP, KT, 64 * W, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
     if (first < keys.hi) {
       ks.load(first);
       vs.load(first);
@@ -1459,10 +1459,24 @@ uint32_t grid_of(AttnParams& p) {
   return (uint32_t)(p.spread ? (p.pairs + 7) / 8 * 8 : p.pairs) * (uint32_t)p.tiles * (uint32_t)p.splits;
 }
 
+// Workgroups of eight waves, 256 rows, with 128 channels of 16 bits, where they fill
+// the compute units: tiles are fetched half as often, and a thread holds half as much
+// of the next one (4096 causal frames of 8 items and 16 heads 669 -> 655 us, a training
+// pass over 4 items and 8 heads 1144 -> 1106; with 64 channels 5 short documents an
+// item 177 -> 224).
+template <class T, int DP> constexpr bool kWide = sizeof(T) == 2 && DP == 128;
+bool wide_rows(int32_t pairs, int32_t rows) { return (int64_t)((rows + 255) / 256) * pairs >= 256; }
+
 template <class T, int DP> hipError_t forward(AttnParams p, const AttnPlan& plan, hipStream_t stream) {
   const uint32_t grid = grid_of(p);
   if (!plan.small) {
-    hipLaunchKernelGGL((mas_attention_rows<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+    if constexpr (kWide<T, DP>) {
+      if (plan.waves == 8) {
+        hipLaunchKernelGGL((mas_attention_rows<T, DP, 8>), dim3(grid), dim3(512), 0, stream, p);
+        return hipGetLastError();
+      }
+    }
+    hipLaunchKernelGGL((mas_attention_rows<T, DP, 4>), dim3(grid), dim3(256), 0, stream, p);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((mas_attention_keys<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
@@ -1479,12 +1493,17 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
   // 64 channels, bf16, with dk, dv: 128 workgroups 53.4 / 44.4 us, 256 60.5 / 62.8).
   p.tiles = (p.rows + 127) / 128;
   const bool few_rows = (int64_t)p.tiles * p.pairs < 256;
+  const bool wide = kWide<T, DP> && wide_rows(p.pairs, p.rows);
   if (few_rows) p.tiles = (p.rows + 31) / 32;
+  if (wide) p.tiles = (p.rows + 255) / 256;
   uint32_t grid = grid_of(p);
-  if (few_rows)
-    hipLaunchKernelGGL((mas_attention_dq<T, DP, true>), dim3(grid), dim3(kThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL((mas_attention_dq<T, DP, false>), dim3(grid), dim3(kThreads), 0, stream, p);
+  if (few_rows) {
+    hipLaunchKernelGGL((mas_attention_dq<T, DP, true, 4>), dim3(grid), dim3(256), 0, stream, p);
+  } else if (!wide) {
+    hipLaunchKernelGGL((mas_attention_dq<T, DP, false, 4>), dim3(grid), dim3(256), 0, stream, p);
+  } else {
+    if constexpr (kWide<T, DP>) hipLaunchKernelGGL((mas_attention_dq<T, DP, false, 8>), dim3(grid), dim3(512), 0, stream, p);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 2) {
@@ -1517,6 +1536,7 @@ template <class T, class F> hipError_t by_width(int D, F&& f) {
 
 AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32) {
   AttnPlan a;
+  a.waves = 4;
   a.splits = 1;
   a.span = Tk;
   a.tiles = (rows + 127) / 128;
@@ -1529,7 +1549,13 @@ AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool
   // 45.2 / 29.2, 256 49.4 / 49.1.  Up to 32 rows always the latter (64 caches of 4096
   // keys, 4 heads: 128 / 43; 512 of 1024 keys 25.7 / 26.1; 2048 of 256 keys 32.3 / 37.6).
   a.small = rows <= 32 || (int64_t)a.tiles * pairs < (fp32 || D <= 64 ? 256 : 128);
-  if (!a.small) return a;
+  if (!a.small) {
+    if (!fp32 && D > 96 && wide_rows(pairs, rows)) {
+      a.waves = 8;
+      a.tiles = (rows + 255) / 256;
+    }
+    return a;
+  }
   a.tiles = (rows + 31) / 32;
   // The keys are split until two workgroups a compute unit are there, into parts of at
   // least 512, four blocks a wave; steps over more than 1024 keys into parts of 128.
