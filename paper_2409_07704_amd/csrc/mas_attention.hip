@@ -95,14 +95,14 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// tanh(x).  exp form: absolute error of about 2^-23; where that is not enough
-// next to x itself (fp32 inputs, |x| < 1/4) the Taylor sum up to x^9, whose next
-// term is below 2^-26 of x there.
-template <class T> __device__ __forceinline__ float tanh_of(float x) {
-  const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2E));
+// tanh(x).  exp form: absolute error of about 2^-23; where that is not enough next to
+// x itself (fp32 inputs, |x| < 1/4) the Taylor sum up to x^9, whose next term is below
+// 2^-26 of x there.  x is a product times `pre`; twice_pre: 2 pre in powers of two.
+template <class T> __device__ __forceinline__ float tanh_of(float product, float pre, float twice_pre) {
+  const float e = __builtin_amdgcn_exp2f(product * twice_pre);
   const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f);
   if constexpr (std::is_same<T, float>::value) {
-    const float y = x * x;
+    const float x = product * pre, y = x * x;
     float s = fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f);
     s = fmaf(y, s, 2.0f / 15.0f);
     s = fmaf(y, s, -1.0f / 3.0f);
@@ -444,7 +444,7 @@ __device__ __forceinline__ Seen seen(int lo, int hi, int k, int n) {
 // From products to scores, in powers of two: x mul - slope distance, with x the
 // product, or tanh(product pre) with a cap.
 struct ScoreRule {
-  float pre, mul;
+  float pre, twice_pre, mul;
   bool capped, sloped;
 };
 __device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
@@ -452,6 +452,7 @@ __device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
   s.capped = p.cap > 0.0f;
   s.sloped = p.slope != nullptr;
   s.pre = s.capped ? p.scale / p.cap : 1.0f;
+  s.twice_pre = s.pre * (2.0f * kLog2E);
   s.mul = (s.capped ? p.cap : p.scale) * kLog2E;
   return s;
 }
@@ -496,7 +497,7 @@ template <class T, int DP> struct Forward {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = tanh_of<T>(s[n][r] * rule.pre);
+        for (int r = 0; r < 16; ++r) s[n][r] = tanh_of<T>(s[n][r], rule.pre, rule.twice_pre);
     }
     if (general) {
 #pragma unroll
@@ -599,7 +600,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
       for (int r = 0; r < 16; ++r) {
         const int at = k0 + acc_row(r, half);
         const bool sees = (at >= w.lo) & (at < w.hi);
-        float x = rule.capped ? tanh_of<T>(s[r] * rule.pre) : s[r];
+        float x = rule.capped ? tanh_of<T>(s[r], rule.pre, rule.twice_pre) : s[r];
         x = fmaf(-w.slope, fabsf((float)(w.at - at)), x * rule.mul);
         s[r] = sees ? x : -INFINITY;
         top = fmaxf(top, s[r]);
@@ -926,7 +927,7 @@ template <class T, int DP> struct BackwardQ {
       if (rule.capped) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = tanh_of<T>(s[r] * rule.pre);
+          s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
           dp[r] *= fmaf(-s[r], s[r], 1.0f);
         }
       }
@@ -1125,7 +1126,7 @@ template <class T, int DP> struct BackwardK {
     if (rule.capped) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = tanh_of<T>(s[r] * rule.pre);
+        s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
         dp[r] *= fmaf(-s[r], s[r], 1.0f);
       }
     }
@@ -1385,7 +1386,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
         if (rule.capped) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = tanh_of<T>(s[r] * rule.pre);
+            s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
             bend[r] = fmaf(-s[r], s[r], 1.0f);
           }
         }
