@@ -305,11 +305,11 @@ typedef struct mas_heads {
  * whatever it holds; nor does a hidden key or value influence `out` and the
  * log-sum-exp, infinities and NaN included.  (In the backward pass, an infinity
  * or NaN inside the lengths may reach gradients of its neighbours.)
- * Precision: sums, maxima and totals in fp32; in the 16-bit types p and ds are
- * rounded to the type before they are multiplied (fp16: as for its gradients
- * at large, values below 6e-8 are lost, so scale the loss); results are
- * rounded once.  MAS_F32 multiplies in fp32.  Repeated calls give identical
- * bits.
+ * Precision: sums, maxima and totals in fp32.  In the 16-bit types p is rounded
+ * to the type before it is multiplied, the gradients of the scores in two
+ * parts (about twice the type's digits; in fp16 values below 6e-8 are lost, so
+ * scale the loss); results are rounded once.  MAS_F32 multiplies in fp32.
+ * Repeated calls give identical bits.
  */
 typedef struct mas_attention_desc {
   int32_t B, Tq, Tk, Hq, Hk, D;
