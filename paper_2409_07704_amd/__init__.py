@@ -1,8 +1,9 @@
 """libmas: batched Monotonic Alignment Search for AMD MI355X (gfx950).
 
-The alignment runs in hand-written HIP kernels behind the C ABI of
-``include/mas.h``; this package is the thin Python binding with the same
-entry-point names.  It never computes an alignment in Python.
+The alignment, and the attention, norm and loss around it, run in hand-written
+HIP kernels behind the C ABI of ``include/mas.h``; this package is the thin
+Python binding with the same entry-point names.  It never computes a result in
+Python.
 """
 from ._native import (  # noqa: F401
     ITEM_BAD_WORKSPACE,
