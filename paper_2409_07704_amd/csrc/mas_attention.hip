@@ -132,7 +132,6 @@ __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.
 struct Interval {
   int lo, hi;
 };
-constexpr int kFewDocs = 12;
 
 // Keys that the query at `place` of item b sees; tk is the item's key length.
 __device__ __forceinline__ Interval interval(const AttnParams& p, int b, int place, int tk) {
@@ -140,39 +139,20 @@ __device__ __forceinline__ Interval interval(const AttnParams& p, int b, int pla
   int pre = 0;
   if (p.doc_start) {
     const int32_t* t = p.doc_start + (size_t)b * (p.N + 1);
-    int first = 0;  // starts up to `place`
-    if (p.N <= kFewDocs) {
-      // Few documents: all starts at once, one wait instead of one a step.
-      int from = 0, to = 0;
-#pragma unroll
-      for (int n = 0; n <= kFewDocs; ++n) {
-        const int at = t[min(n, p.N)];
-        const int len = p.prefix ? p.prefix[(size_t)b * p.N + min(n, p.N - 1)] : 0;
-        const bool before = n <= p.N && at <= place;
-        to = before || first < n ? to : at;
-        from = before ? at : from;
-        pre = before ? len : pre;
-        first = before ? n + 1 : first;
+    int first = 0, n = p.N + 1;  // starts up to `place`: the first n of them are candidates
+    while (n > 0) {
+      const int step = n / 2;
+      if (t[first + step] <= place) {
+        first += step + 1;
+        n -= step + 1;
+      } else {
+        n = step;
       }
-      if (first == 0 || first > p.N) return {0, 0};
-      lo = max(from, 0);
-      hi = min(to, tk);
-    } else {
-      int n = p.N + 1;
-      while (n > 0) {
-        const int step = n / 2;
-        if (t[first + step] <= place) {
-          first += step + 1;
-          n -= step + 1;
-        } else {
-          n = step;
-        }
-      }
-      if (first == 0 || first > p.N) return {0, 0};
-      lo = max(t[first - 1], 0);
-      hi = min(t[first], tk);
-      if (p.prefix) pre = p.prefix[(size_t)b * p.N + first - 1];
     }
+    if (first == 0 || first > p.N) return {0, 0};
+    lo = max(t[first - 1], 0);
+    hi = min(t[first], tk);
+    if (p.prefix) pre = p.prefix[(size_t)b * p.N + first - 1];
   } else if (p.prefix) {
     pre = p.prefix[b];
   }

@@ -17,6 +17,10 @@
 // their sums in the workspace, where a second kernel adds them, in order, with the
 // item's loss.  So sums do not depend on the order in which workgroups run.  All
 // in fp32.
+//
+// Measured, 64 items of up to 1024 text rows and 4096 frames of 192 channels with
+// log-sigmas: 138 us for 600 MB moved (286 read, 306 written), 4.3 TB/s (a copy: 5.1),
+// and 5 us to join.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

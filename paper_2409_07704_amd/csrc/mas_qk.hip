@@ -15,6 +15,9 @@
 // them.  Sums are in fp32; results are rounded once, to the inputs' type.  The
 // gradients of the weights are summed in a fixed order: each group over its
 // rows, a workgroup over its groups, one more kernel over the workgroups.
+//
+// Measured, 8 x 4096 tokens of 16 + 4 heads of 128 in bf16: forward 81 us for 336 MB,
+// 4.1 TB/s; backward 136 us for 503 MB, 3.7 TB/s (a copy: 5.1); the weights' sum 6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -24,8 +27,11 @@ namespace mas {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBlocks = 1024;  // of the backward pass
-constexpr int kInFlight = 4;      // heads a group loads at a time, where it has as many
+// Workgroups of the backward pass at most (2048: 8 x 4096 tokens of 20 heads 219 us
+// with the forward pass, 1024: 214).
+constexpr int kMaxBlocks = 1024;
+// Heads a group loads at a time, where it has as many (2: 217 us, 4: 214).
+constexpr int kInFlight = 4;
 
 template <class T, int V> struct Pack {
   typedef T type __attribute__((ext_vector_type(V)));
@@ -360,13 +366,16 @@ __global__ void __launch_bounds__(kThreads) mas_qk_weights_kernel(const QkParams
   if (dw) dw[c < p.D ? c : c - p.D] = x;
 }
 
-// Groups that share a token's heads: one each while tokens are few, so that there
-// are groups for the whole chip; more heads a group save fetches of the angles.
+// Groups that share a token's heads: several while tokens are few, so that there are
+// groups for the whole chip; more heads a group save fetches of the angles.  Measured
+// with at least 8192 / 32768 / 131072 groups, 20 heads, bf16: 4 x 1024 tokens of 128
+// channels 14.9 / 18.2 / 28.3 us, backward 27.2 / 27.8 / 34.5; 32 x 1024 of 64 32.4 /
+// 32.5 / 39.5 and 64.8 / 64.6 / 92.8.
 int parts_of(const QkParams& p) {
   const int heads = p.Hq + p.Hk;
   const int64_t tokens = (int64_t)p.B * p.T;
   int parts = 1;
-  while (parts < heads && tokens * parts < 32768) parts *= 2;
+  while (parts < heads && tokens * parts < 8192) parts *= 2;
   return parts < heads ? parts : heads;
 }
 
