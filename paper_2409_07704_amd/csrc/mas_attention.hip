@@ -173,16 +173,17 @@ struct Place {
   int pair, tile, split;
   bool idle;
 };
-__device__ __forceinline__ Place place_of(const AttnParams& p) {
-  const uint32_t per = (uint32_t)p.tiles * (uint32_t)p.splits;
-  uint32_t pair = blockIdx.x / per, rest = blockIdx.x % per;
+__device__ __forceinline__ Place place_of(const AttnParams& p, uint32_t block, int tiles) {
+  const uint32_t per = (uint32_t)tiles * (uint32_t)p.splits;
+  uint32_t pair = block / per, rest = block % per;
   if (p.spread) {
-    const uint32_t n = blockIdx.x / 8;
-    pair = n / per * 8 + blockIdx.x % 8;
+    const uint32_t n = block / 8;
+    pair = n / per * 8 + block % 8;
     rest = n % per;
   }
-  return {(int)pair, (int)(rest % (uint32_t)p.tiles), (int)(rest / (uint32_t)p.tiles), pair >= (uint32_t)p.pairs};
+  return {(int)pair, (int)(rest % (uint32_t)tiles), (int)(rest / (uint32_t)tiles), pair >= (uint32_t)p.pairs};
 }
+__device__ __forceinline__ Place place_of(const AttnParams& p) { return place_of(p, blockIdx.x, p.tiles); }
 
 template <class T> __device__ __forceinline__ const T* head(const HeadView& v, int b, int h) {
   return reinterpret_cast<const T*>(v.data) + (int64_t)b * v.sb + (int64_t)h * v.sh;
@@ -953,93 +954,75 @@ template <class T, int DP> struct BackwardQ {
   }
 };
 
-// FEW: 32 rows a workgroup, its four waves take the blocks of keys in turn; else W
-// waves of 32 rows with shared tiles, as in the forward pass.
-template <class T, int DP, bool FEW, int W>
-__global__ void __launch_bounds__(64 * W, FEW || sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2) mas_attention_dq(const AttnParams p) {
-  constexpr int KT = FEW ? 32 : kTile<T>, LD = kLd<T, DP>, SETS = FEW ? kWaves : 2;
-  __shared__ __align__(16) T kt[SETS][KT * LD];
-  __shared__ __align__(16) T vt[SETS][KT * LD];
+// What a wave's rows need before their keys: queries, gradients, statistics.  KEEP:
+// the kernel of dk and dv will want them.
+template <class T, int DP, bool KEEP>
+__device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& f, const Rows& w, int pair, int b, int hk, int lane, bool first) {
+  load_q<T, DP>(p, p.q, w, b, lane, f.q);
+  load_q<T, DP>(p, p.dout, w, b, lane, f.g);
+  f.delta = 0.0f;
+  const T* row = head<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st;
+#pragma unroll
+  for (int c = 0; c < DP / 16; ++c) {
+    const frag<T> o = w.used ? load_frag(row, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.delta = fmaf((float)o[e], (float)f.g[c][e], f.delta);
+  }
+  f.delta = add_halves(f.delta);
+  f.lse = w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f;
+  if (KEEP && w.in && lane < 32 && first) {
+    p.stat[(size_t)pair * p.rows + w.row] = float2{f.lse, f.delta};
+    if (hk == 0 && w.row == w.tok * p.G) p.see[(size_t)b * p.Tq + w.tok] = int2{w.lo, w.hi};
+  }
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) f.dq[d] = f32x16(0.0f);
+}
+template <class T, int DP> __device__ __forceinline__ void store_dq(const AttnParams& p, const BackwardQ<T, DP>& f, const Rows& w, int b, int lane) {
+  if (w.in) store_row<T, DP>(head_out<T>(p.dq, b, w.h) + (int64_t)w.tok * p.dq.st, f.dq, w.hi > w.lo ? p.scale : 0.0f, lane / 32, p.D, p.vec);
+}
+
+// W waves of 32 rows with shared tiles, as in the forward pass.
+template <class T, int DP, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2) mas_attention_dq(const AttnParams p) {
+  constexpr int KT = kTile<T>, LD = kLd<T, DP>;
+  __shared__ __align__(16) T kt[2][KT * LD];
+  __shared__ __align__(16) T vt[2][KT * LD];
   __shared__ int range[2 * kMaxWaves];
-  static_assert(!FEW || sizeof(kt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
   const Place at = place_of(p);
   if (at.idle) return;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
-  const Rows w = rows_of(p, FEW ? 32 * tile + lane % 32 : 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
+  const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
   const ScoreRule rule = score_rule(p);
-
   BackwardQ<T, DP> f;
-  load_q<T, DP>(p, p.q, w, b, lane, f.q);
-  load_q<T, DP>(p, p.dout, w, b, lane, f.g);
-  f.delta = 0.0f;
-  {
-    const T* row = head<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st;
-#pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-      const frag<T> o = w.used ? load_frag(row, 16 * c + 8 * (lane / 32), p.D, p.vec) : frag<T>(0);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f.delta = fmaf((float)o[e], (float)f.g[c][e], f.delta);
-    }
-    f.delta = add_halves(f.delta);
-  }
-  f.lse = w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f;
-  if (w.in && lane < 32 && (!FEW || wave == 0)) {
-    p.stat[(size_t)at.pair * p.rows + w.row] = float2{f.lse, f.delta};
-    if (hk == 0 && w.row == w.tok * p.G) p.see[(size_t)b * p.Tq + w.tok] = int2{w.lo, w.hi};
-  }
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) f.dq[d] = f32x16(0.0f);
-
+  start_dq<T, DP, true>(p, f, w, at.pair, b, hk, lane, true);
   const int first = keys.lo / KT * KT;
-  if constexpr (FEW) {
-    Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
-    int k0 = first + 32 * wave;
-    if (k0 < keys.hi) {
-      ks.load(k0);
-      vs.load(k0);
+  Stage<T, DP, KT, 64 * W, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
+  if (first < keys.hi) {
+    ks.load(first);
+    vs.load(first);
+    ks.store(kt[0], LD);
+    vs.store(vt[0], LD);
+  }
+  __syncthreads();
+  int cur = 0;
+  for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
+    const bool more = k0 + KT < keys.hi;
+    if (more) {
+      ks.load(k0 + KT);
+      vs.load(k0 + KT);
     }
-    for (; k0 < keys.hi; k0 += 32 * kWaves) {
-      ks.store(kt[wave], LD);
-      vs.store(vt[wave], LD);
-      wave_sync();
-      if (k0 + 32 * kWaves < keys.hi) {
-        ks.load(k0 + 32 * kWaves);
-        vs.load(k0 + 32 * kWaves);
-      }
-      f.template step<1>(kt[wave], vt[wave], LD, k0, w, rule, lane);
-      wave_sync();
-    }
-    add_waves<kWaves>(f.dq, reinterpret_cast<float*>(kt), wave, lane);
-    if (wave > 0) return;
-  } else {
-    Stage<T, DP, KT, 64 * W, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
-    if (first < keys.hi) {
-      ks.load(first);
-      vs.load(first);
-      ks.store(kt[0], LD);
-      vs.store(vt[0], LD);
+    f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
+    if (more) {
+      ks.store(kt[cur ^ 1], LD);
+      vs.store(vt[cur ^ 1], LD);
     }
     __syncthreads();
-    int cur = 0;
-    for (int k0 = first; k0 < keys.hi; k0 += KT, cur ^= 1) {
-      const bool more = k0 + KT < keys.hi;
-      if (more) {
-        ks.load(k0 + KT);
-        vs.load(k0 + KT);
-      }
-      f.template step<KT / 32>(kt[cur], vt[cur], LD, k0, w, rule, lane);
-      if (more) {
-        ks.store(kt[cur ^ 1], LD);
-        vs.store(vt[cur ^ 1], LD);
-      }
-      __syncthreads();
-    }
   }
-  if (w.in) store_row<T, DP>(head_out<T>(p.dq, b, w.h) + (int64_t)w.tok * p.dq.st, f.dq, w.hi > w.lo ? p.scale : 0.0f, lane / 32, p.D, p.vec);
+  store_dq(p, f, w, b, lane);
 }
 
 // What a row brings along: its statistics and the keys it sees.  Loaded without
@@ -1056,6 +1039,23 @@ struct RowInfo {
     stat = p.stat[((size_t)b * p.Hk + hk) * p.rows + i];
     see = p.see[(size_t)b * p.Tq + tok];
     slope = p.slope ? p.slope[hk * p.G + i - tok * p.G] : 0.0f;
+  }
+  // The same from the tensors themselves: rows r and, in the lanes 32 on, r again.
+  template <class T> __device__ __forceinline__ void make(const AttnParams& p, int b, int hk, int r, int tq, int tk, int lane) {
+    const Rows w = rows_of(p, r, b, hk, tq, tk);
+    row = r;
+    tok = w.tok;
+    see = int2{w.lo, w.hi};
+    slope = p.slope ? p.slope[w.h] : 0.0f;
+    float delta = 0.0f;
+    const T* o = head<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st;
+    const T* g = head<T>(p.dout, b, w.h) + (int64_t)w.tok * p.dout.st;
+    for (int c = 8 * (lane / 32); c < p.D; c += 16) {
+      const frag<T> x = w.used ? load_frag(o, c, p.D, p.vec) : frag<T>(0), y = w.used ? load_frag(g, c, p.D, p.vec) : frag<T>(0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)x[e], (float)y[e], delta);
+    }
+    stat = float2{w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f, add_halves(delta)};
   }
 };
 template <int ROWS> struct RowTable {
@@ -1171,11 +1171,18 @@ template <class T, int DP> struct BackwardK {
 };
 
 // The rows that see any of the n keys from kb0 on.
+template <bool OWN = false>
 __device__ __forceinline__ Interval rows_seeing(const AttnParams& p, int b, int tq, int kb0, int n, int tk, int (&range)[2 * kMaxWaves]) {
   int lo = 0x7fffffff, hi = 0;
   if (kb0 < tk) {
     for (int t = threadIdx.x; t < tq; t += blockDim.x) {
-      const int2 s = p.see[(size_t)b * p.Tq + t];
+      int2 s;
+      if (OWN) {
+        const Interval v = interval(p, b, t + tk - tq, tk);
+        s = int2{v.lo, v.hi};
+      } else {
+        s = p.see[(size_t)b * p.Tq + t];
+      }
       if (s.x < kb0 + n && s.y > kb0) {
         lo = min(lo, t);
         hi = t + 1;
@@ -1194,58 +1201,125 @@ template <class T, int DP> __device__ __forceinline__ void store_keys(const Attn
   store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, 1.0f, lane / 32, p.D, p.vec);
 }
 
-// Few keys, and fp32: 32 keys a workgroup, whose four waves take the blocks of 32
-// rows in turn; their sums are added at the end.
-template <class T, int DP>
-__global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
+// Few rows or keys, and all keys in fp32: 32 of them a workgroup, whose four waves take
+// the blocks of 32 of the others in turn; their sums are added at the end.
+template <class T, int DP> struct FewLds {
+  static constexpr int LD = kLd<T, DP>;
+  T a[kWaves][32 * LD], b[kWaves][32 * LD];
+  RowTable<32> table[kWaves];
+  int range[2 * kMaxWaves];
+  static_assert(sizeof(T) * 32 * LD * kWaves >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
+};
+
+template <class T, int DP, bool KEEP> __device__ __forceinline__ void few_rows(const AttnParams& p, const Place& at, int tiles, FewLds<T, DP>& lds) {
+  constexpr int LD = kLd<T, DP>;
+  const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
+  const int tile = p.causal ? tiles - 1 - at.tile : at.tile;
+  const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
+  const Interval keys = key_range(w.lo, w.hi, lds.range);
+  const ScoreRule rule = score_rule(p);
+  BackwardQ<T, DP> f;
+  start_dq<T, DP, KEEP>(p, f, w, at.pair, b, hk, lane, wave == 0);
+  Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
+  int k0 = keys.lo / 32 * 32 + 32 * wave;
+  if (k0 < keys.hi) {
+    ks.load(k0);
+    vs.load(k0);
+  }
+  for (; k0 < keys.hi; k0 += 32 * kWaves) {
+    ks.store(lds.a[wave], LD);
+    vs.store(lds.b[wave], LD);
+    wave_sync();
+    if (k0 + 32 * kWaves < keys.hi) {
+      ks.load(k0 + 32 * kWaves);
+      vs.load(k0 + 32 * kWaves);
+    }
+    f.template step<1>(lds.a[wave], lds.b[wave], LD, k0, w, rule, lane);
+    wave_sync();
+  }
+  add_waves<kWaves>(f.dq, reinterpret_cast<float*>(lds.a), wave, lane);
+  if (wave == 0) store_dq(p, f, w, b, lane);
+}
+
+// OWN: without the statistics and intervals of another kernel.
+template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(const AttnParams& p, const Place& at, FewLds<T, DP>& lds) {
   constexpr int LD = kLd<T, DP>;
   // Products take so long in fp32 that the next tile need not be fetched meanwhile,
   // for which there are no registers.
   constexpr bool kAhead = sizeof(T) == 2;
-  __shared__ __align__(16) T qt[kWaves][32 * LD];
-  __shared__ __align__(16) T gt[kWaves][32 * LD];
-  __shared__ __align__(16) RowTable<32> table[kWaves];
-  __shared__ int range[2 * kMaxWaves];
-  static_assert(sizeof(qt) >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
-  const Place at = place_of(p);
-  if (at.idle) return;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const int k0 = 32 * at.tile, key = k0 + lane % 32;
-  const Interval rows = rows_seeing(p, b, tq, k0, 32, tk, range);
+  const Interval rows = rows_seeing<OWN>(p, b, tq, k0, 32, tk, lds.range);
   const ScoreRule rule = score_rule(p);
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
   Stage<T, DP, 32, 64, true> qs(p, p.q, b, hk, tq * p.G, lane), gs(p, p.dout, b, hk, tq * p.G, lane);
   RowInfo info;
-  const auto fetch = [&](int r) {
-    info.load(p, b, hk, r + lane % 32);
-    qs.load(r);
-    gs.load(r);
+  const auto learn = [&](int r) {
+    if (OWN)
+      info.make<T>(p, b, hk, r + lane % 32, tq, tk, lane);
+    else
+      info.load(p, b, hk, r + lane % 32);
   };
   int r0 = rows.lo / 32 * 32 + 32 * wave;
-  if (kAhead && r0 < rows.hi) fetch(r0);
+  if (kAhead && r0 < rows.hi) {
+    qs.load(r0);
+    gs.load(r0);
+    learn(r0);
+  }
   for (; r0 < rows.hi; r0 += 32 * kWaves) {
     if (kAhead) {
-      qs.store(qt[wave], LD);
-      gs.store(gt[wave], LD);
+      qs.store(lds.a[wave], LD);
+      gs.store(lds.b[wave], LD);
     } else {
-      info.load(p, b, hk, r0 + lane % 32);
       qs.load(r0);
-      qs.store(qt[wave], LD);
+      qs.store(lds.a[wave], LD);
       gs.load(r0);
-      gs.store(gt[wave], LD);
+      gs.store(lds.b[wave], LD);
+      learn(r0);
     }
-    if (lane < 32) table[wave].put(lane, info, tk - tq, rows.hi);
+    if (lane < 32) lds.table[wave].put(lane, info, tk - tq, rows.hi);
     wave_sync();
-    if (kAhead && r0 + 32 * kWaves < rows.hi) fetch(r0 + 32 * kWaves);
-    f.step(qt[wave], gt[wave], LD, table[wave], 0, k0, rule, lane);
+    const int next = r0 + 32 * kWaves;
+    if (kAhead && next < rows.hi) {
+      qs.load(next);
+      gs.load(next);
+      learn(next);
+    }
+    f.step(lds.a[wave], lds.b[wave], LD, lds.table[wave], 0, k0, rule, lane);
     wave_sync();
   }
-  add_waves<kWaves>(f.dk, reinterpret_cast<float*>(qt), wave, lane);
-  add_waves<kWaves>(f.dv, reinterpret_cast<float*>(qt), wave, lane);
+  add_waves<kWaves>(f.dk, reinterpret_cast<float*>(lds.a), wave, lane);
+  add_waves<kWaves>(f.dv, reinterpret_cast<float*>(lds.a), wave, lane);
   if (wave == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
+}
+
+template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dq_few(const AttnParams p) {
+  __shared__ __align__(16) FewLds<T, DP> lds;
+  const Place at = place_of(p);
+  if (!at.idle) few_rows<T, DP, true>(p, at, p.tiles, lds);
+}
+
+template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
+  __shared__ __align__(16) FewLds<T, DP> lds;
+  const Place at = place_of(p);
+  if (!at.idle) few_keys<T, DP, false>(p, at, lds);
+}
+
+// Both at once, the first `split` workgroups for dq, where neither fills the chip.
+template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_attention_few_backward(const AttnParams p, uint32_t split, int row_tiles, int key_tiles) {
+  __shared__ __align__(16) FewLds<T, DP> lds;
+  const bool by_rows = blockIdx.x < split;
+  const Place at = place_of(p, by_rows ? blockIdx.x : blockIdx.x - split, by_rows ? row_tiles : key_tiles);
+  if (at.idle) return;
+  if (by_rows)
+    few_rows<T, DP, false>(p, at, row_tiles, lds);
+  else
+    few_keys<T, DP, true>(p, at, lds);
 }
 
 // 16-bit types: 64 keys a workgroup, two waves by keys and two by rows, which
@@ -1490,23 +1564,40 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
   p.tiles = (p.rows + 127) / 128;
   const bool few_rows = (int64_t)p.tiles * p.pairs < 256;
   const bool wide = kWide<T, DP> && wide_rows(p.pairs, p.rows);
+  // 64 keys a workgroup where those fill the compute units, else 32 (512 keys of 64
+  // channels, bf16, with dq: 128 workgroups of 64 keys 28.3 / 25.4 us, 256 30.9 / 38.4).
+  const int key_tiles = (p.Tk + 63) / 64;
+  const bool few_keys = sizeof(T) == 4 || (int64_t)key_tiles * p.pairs < 256;
+  // One launch where the workgroups of both find a compute unit of their own, else one
+  // after the other (256 workgroups against two launches of 128: 64 channels bf16 18.6 /
+  // 22.4 us, 96 channels fp32 26.8 / 36.0; 512 against 256 and 256: 27.2 / 22.7, 42.5 / 36.8).
+  if (few_rows && few_keys) {
+    const int rows = (p.rows + 31) / 32, keys = (p.Tk + 31) / 32;
+    p.tiles = rows;
+    const uint32_t split = grid_of(p);
+    p.tiles = keys;
+    const uint32_t both = split + grid_of(p);
+    if (both <= 256) {
+      hipLaunchKernelGGL((mas_attention_few_backward<T, DP>), dim3(both), dim3(kThreads), 0, stream, p, split, rows, keys);
+      return hipGetLastError();
+    }
+    p.tiles = (p.rows + 127) / 128;
+  }
   if (few_rows) p.tiles = (p.rows + 31) / 32;
   if (wide) p.tiles = (p.rows + 255) / 256;
   uint32_t grid = grid_of(p);
   if (few_rows) {
-    hipLaunchKernelGGL((mas_attention_dq<T, DP, true, 4>), dim3(grid), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((mas_attention_dq_few<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
   } else if (!wide) {
-    hipLaunchKernelGGL((mas_attention_dq<T, DP, false, 4>), dim3(grid), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((mas_attention_dq<T, DP, 4>), dim3(grid), dim3(256), 0, stream, p);
   } else {
-    if constexpr (kWide<T, DP>) hipLaunchKernelGGL((mas_attention_dq<T, DP, false, 8>), dim3(grid), dim3(512), 0, stream, p);
+    if constexpr (kWide<T, DP>) hipLaunchKernelGGL((mas_attention_dq<T, DP, 8>), dim3(grid), dim3(512), 0, stream, p);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 2) {
-    // 64 keys a workgroup where those fill the compute units, else 32 (512 keys of 64
-    // channels, bf16, with dq: 128 workgroups of 64 keys 28.3 / 25.4 us, 256 30.9 / 38.4).
-    p.tiles = (p.Tk + 63) / 64;
-    if ((int64_t)p.tiles * p.pairs >= 256) {
+    if (!few_keys) {
+      p.tiles = key_tiles;
       grid = grid_of(p);
       if constexpr (DP > 64)
         hipLaunchKernelGGL((mas_attention_dkv_pairs<T, DP>), dim3(grid), dim3(2 * kThreads), 0, stream, p);

@@ -81,6 +81,14 @@ def test_shared_heads(mas, Hq, Hk):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B", [20, 30])
+def test_gradients_in_one_launch_and_in_two(mas, dtype, B):
+    """Few items: 40 pairs of 3 blocks of rows and 3 of keys, 240 workgroups; and 60, 360."""
+    lens = _ints([96, 0, 1, 33, 65] * (B // 5))
+    run_and_check(mas, *make(B, 96, 96, 2, 2, 72, dtype, B), "launches", t_q=lens, t_k=lens, causal=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("big", [False, True])
 def test_masks_and_biases(mas, dtype, big):
     """Documents, prefixes, caps and distances together, on a few items (waves take
