@@ -109,13 +109,17 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// tanh(x).  exp form: absolute error of about 2^-23; where that is not enough next to
-// x itself (fp32 inputs, |x| < 1/4) the Taylor sum up to x^9, whose next term is below
-// 2^-26 of x there.  x is a product times `pre`; twice_pre: 2 pre in powers of two.
-template <class T> __device__ __forceinline__ float tanh_of(float product, float pre, float twice_pre) {
+// A capped score by way of r = -1 / (e^2x + 1): tanh(x) = 1 + 2 r, whose last step the
+// next factor takes along, and tanh'(x) = -4 (r + r r).  The absolute error of about 2^-23
+// in tanh is not enough next to x itself in fp32 with |x| < 1/4: there the Taylor sum up
+// to x^9, whose next term is below 2^-26 of x, and in fp32 tanh itself in r's place.  x is
+// a product times `pre`; twice_pre: 2 pre in powers of two.
+template <class T> constexpr bool kByHalf = sizeof(T) == 2;
+template <class T> __device__ __forceinline__ float bent(float product, float pre, float twice_pre) {
   const float e = __builtin_amdgcn_exp2f(product * twice_pre);
-  const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f);
-  if constexpr (std::is_same<T, float>::value) {
+  const float r = __builtin_amdgcn_rcpf(-1.0f - e);
+  if constexpr (!kByHalf<T>) {
+    const float t = fmaf(2.0f, r, 1.0f);
     const float x = product * pre, y = x * x;
     float s = fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f);
     s = fmaf(y, s, 2.0f / 15.0f);
@@ -123,8 +127,10 @@ template <class T> __device__ __forceinline__ float tanh_of(float product, float
     s = fmaf(y * s, x, x);
     return fabsf(x) < 0.25f ? s : t;
   }
-  return t;
+  return r;
 }
+// tanh', without its factor 4 where r stands for tanh.
+template <class T> __device__ __forceinline__ float bend_of(float x) { return fmaf(-x, x, kByHalf<T> ? -x : 1.0f); }
 
 // 1 / l, and 0 where nothing was summed; NaN stays.
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -439,19 +445,32 @@ __device__ __forceinline__ Seen seen(int lo, int hi, int k, int n) {
 
 // From products to scores, in powers of two: x mul - slope distance, with x the
 // product, or tanh(product pre) with a cap.
+// That is mul x + add of the product, or of what `bent` makes of it, and the forward
+// pass brings `add` in with the log-sum-exp.  lift: added to the exponent where tanh'
+// lacks its factor 4, so that ds has it (and p, until dv is stored).
 struct ScoreRule {
-  float pre, twice_pre, mul;
+  float pre, twice_pre, mul, add, lift;
   bool capped, sloped;
 };
-__device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
+template <class T> __device__ __forceinline__ float score_add(const AttnParams& p) { return kByHalf<T> && p.cap > 0.0f ? p.cap * kLog2E : 0.0f; }
+template <class T> __device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
   ScoreRule s;
   s.capped = p.cap > 0.0f;
   s.sloped = p.slope != nullptr;
   s.pre = s.capped ? p.scale / p.cap : 1.0f;
   s.twice_pre = s.pre * (2.0f * kLog2E);
   s.mul = (s.capped ? p.cap : p.scale) * kLog2E;
+  s.add = score_add<T>(p);
+  s.lift = 0.0f;
+  if (kByHalf<T> && s.capped) {
+    s.mul *= 2.0f;
+    s.lift = 2.0f;
+  }
   return s;
 }
+
+// What undoes `lift`.
+template <class T> __device__ __forceinline__ float p_unit(const AttnParams& p) { return kByHalf<T> && p.cap > 0.0f ? 0.25f : 1.0f; }
 
 // ------------------------------------------------------------------ forward
 // Keys of a tile: 64, or 32 in fp32, whose rows are twice as long.
@@ -493,7 +512,7 @@ template <class T, int DP> struct Forward {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = tanh_of<T>(s[n][r], rule.pre, rule.twice_pre);
+        for (int r = 0; r < 16; ++r) s[n][r] = bent<T>(s[n][r], rule.pre, rule.twice_pre);
     }
     if (general) {
 #pragma unroll
@@ -569,7 +588,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
   const int lane = threadIdx.x % 64, half = lane / 32;
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const Rows w = rows_of(p, row, b, hk, tq, tk);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   const T* qr = head<T>(p.q, b, w.h) + (int64_t)w.tok * p.q.st;
   const T* kb = head<T>(p.k, b, hk);
   const T* vb = head<T>(p.v, b, hk);
@@ -596,7 +615,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
       for (int r = 0; r < 16; ++r) {
         const int at = k0 + acc_row(r, half);
         const bool sees = (at >= w.lo) & (at < w.hi);
-        float x = rule.capped ? tanh_of<T>(s[r], rule.pre, rule.twice_pre) : s[r];
+        float x = rule.capped ? bent<T>(s[r], rule.pre, rule.twice_pre) : s[r];
         x = fmaf(-w.slope, fabsf((float)(w.at - at)), x * rule.mul);
         s[r] = sees ? x : -INFINITY;
         top = fmaxf(top, s[r]);
@@ -654,7 +673,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
     part[p.D] = m;
     part[p.D + 1] = l;
   } else if (p.lse) {
-    p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+    p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (m + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
   }
 }
 
@@ -685,7 +704,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 3 : 2) ma
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
 
   Forward<T, DP> f;
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
@@ -720,7 +739,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 3 : 2) ma
   if (w.hi <= w.lo) f.clear();
   const float l = add_halves(f.l);
   store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
-  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (f.m + __builtin_amdgcn_logf(l)) * kLn2;
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (f.m + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
 }
 
 // Few rows: 32 a workgroup, whose four waves take the blocks of 32 keys in turn,
@@ -748,7 +767,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
   Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   keys.lo = max(keys.lo / 32 * 32, at.split * p.span);
   keys.hi = min(keys.hi, (at.split + 1) * p.span);
 
@@ -823,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
     return;
   }
   store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
-  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (top + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
 }
 
 // The parts of a row, joined: a wave for each row, two channels a lane.
@@ -876,7 +895,7 @@ __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams 
 #pragma unroll
   for (int e = 0; e < 2; ++e)
     if (lane + 64 * e < p.D) out[lane + 64 * e] = (T)(mul != 0.0f ? x[e] * mul : 0.0f);
-  if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.Tq + tok] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.Tq + tok] = (top + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
 }
 
 // ----------------------------------------------------------------- backward
@@ -906,7 +925,7 @@ template <int W, int N> __device__ __forceinline__ void add_waves(f32x16 (&x)[N]
 template <class T, int DP> struct BackwardQ {
   frag<T> q[DP / 16], g[DP / 16];  // queries and gradients of the output
   f32x16 dq[DP / 32];
-  float lse, delta;  // lse in powers of two
+  float base, delta;  // base: what the exponent has besides the score's factor
   template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const ScoreRule& rule, int lane) {
     const int half = lane / 32;
 #pragma unroll
@@ -923,12 +942,12 @@ template <class T, int DP> struct BackwardQ {
       if (rule.capped) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
-          dp[r] *= fmaf(-s[r], s[r], 1.0f);
+          s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
+          dp[r] *= bend_of<T>(s[r]);
         }
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], rule.mul, -lse);
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], rule.mul, base);
       if (rule.sloped) {
         const float d = (float)(w.at - k0 - 4 * half);
 #pragma unroll
@@ -957,7 +976,7 @@ template <class T, int DP> struct BackwardQ {
 // What a wave's rows need before their keys: queries, gradients, statistics.  KEEP:
 // the kernel of dk and dv will want them.
 template <class T, int DP, bool KEEP>
-__device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& f, const Rows& w, int pair, int b, int hk, int lane, bool first) {
+__device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& f, const Rows& w, const ScoreRule& rule, int pair, int b, int hk, int lane, bool first) {
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
   load_q<T, DP>(p, p.dout, w, b, lane, f.g);
   f.delta = 0.0f;
@@ -969,9 +988,10 @@ __device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& 
     for (int e = 0; e < 8; ++e) f.delta = fmaf((float)o[e], (float)f.g[c][e], f.delta);
   }
   f.delta = add_halves(f.delta);
-  f.lse = w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f;
+  const float lse = w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f;
+  f.base = rule.add + rule.lift - lse;
   if (KEEP && w.in && lane < 32 && first) {
-    p.stat[(size_t)pair * p.rows + w.row] = float2{f.lse, f.delta};
+    p.stat[(size_t)pair * p.rows + w.row] = float2{lse, f.delta};
     if (hk == 0 && w.row == w.tok * p.G) p.see[(size_t)b * p.Tq + w.tok] = int2{w.lo, w.hi};
   }
 #pragma unroll
@@ -996,9 +1016,9 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   BackwardQ<T, DP> f;
-  start_dq<T, DP, true>(p, f, w, at.pair, b, hk, lane, true);
+  start_dq<T, DP, true>(p, f, w, rule, at.pair, b, hk, lane, true);
   const int first = keys.lo / KT * KT;
   Stage<T, DP, KT, 64 * W, false> ks(p, p.k, b, hk, tk, tid), vs(p, p.v, b, hk, tk, tid);
   if (first < keys.hi) {
@@ -1058,20 +1078,53 @@ struct RowInfo {
     stat = float2{w.hi > w.lo ? p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] * kLog2E : 0.0f, add_halves(delta)};
   }
 };
+// As a table for the workgroup's `keys` keys from kb0 on.  The exponent of a row and
+// a key is mul x + base + slope (key - kb0): distances are linear on one side of the
+// row's place; where the row sees keys on both sides here, those behind `at` take
+// 2 slope (key - at) more off.
 template <int ROWS> struct RowTable {
-  float lse[ROWS], delta[ROWS], slope[ROWS], at[ROWS];
+  float base[ROWS], less[ROWS], slope[ROWS], at[ROWS];  // less: -delta
   int lo[ROWS], hi[ROWS];
   // shift: from a token to its place; rows from `limit` on see nothing.
-  __device__ __forceinline__ void put(int i, const RowInfo& x, int shift, int limit) {
-    lse[i] = x.stat.x;
-    delta[i] = x.stat.y;
-    slope[i] = x.slope * kLog2E;
-    at[i] = (float)(x.tok + shift);
+  __device__ __forceinline__ void put(int i, const RowInfo& x, int shift, int limit, const ScoreRule& rule, int kb0, int keys) {
+    const int place = x.tok + shift, e = place - kb0;
+    const float k = (e > 0 ? x.slope : -x.slope) * kLog2E;
+    base[i] = fmaf(-k, (float)e, rule.add + rule.lift - x.stat.x);
+    less[i] = -x.stat.y;
+    slope[i] = k;
+    at[i] = e > 0 && e < keys - 1 && x.see.y > place + 1 ? (float)e : INFINITY;
     lo[i] = x.row < limit ? x.see.x : 0;
     hi[i] = x.row < limit ? x.see.y : 0;
   }
+  // Scores of rows i + 8 n + 0 ... 3 down the registers and the key kb0 + k, complete.
+  __device__ __forceinline__ void add_to(f32x16& s, int i, int k, bool both_sides, const ScoreRule& rule) const;
 };
 template <class V> __device__ __forceinline__ V four_at(const void* at) { return *reinterpret_cast<const V*>(at); }
+template <int ROWS> __device__ __forceinline__ void RowTable<ROWS>::add_to(f32x16& s, int i, int k, bool both_sides, const ScoreRule& rule) const {
+  if (!rule.sloped) {
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const f32x4 b = four_at<f32x4>(&base[i + 2 * r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, b[e]);
+    }
+    return;
+  }
+  const float place = (float)k;
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) {
+    const f32x4 b = four_at<f32x4>(&base[i + 2 * r]), m = four_at<f32x4>(&slope[i + 2 * r]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, fmaf(m[e], place, b[e]));
+  }
+  if (!both_sides) return;
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) {
+    const f32x4 m = four_at<f32x4>(&slope[i + 2 * r]), where = four_at<f32x4>(&at[i + 2 * r]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[r + e] = fmaf(-2.0f * m[e], fmaxf(place - where[e], 0.0f), s[r + e]);
+  }
+}
 
 // dk, dv of a wave's 32 keys (lane l and l + 32 hold key l % 32): s = q k^T with
 // the rows down the registers, so that p and ds are operands of dv^T = dout^T p
@@ -1091,15 +1144,22 @@ template <class T, int DP> struct BackwardK {
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16(0.0f);
   }
   // Rows i0 ... i0 + 31 of a tile in LDS against the keys from k0 on.
-  template <int ROWS> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int k0, const ScoreRule& rule, int lane) {
-    const int half = lane / 32, key = k0 + lane % 32;
+  template <int ROWS> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int kb0, int k0, const ScoreRule& rule, int lane) {
+    const int half = lane / 32, key = k0 + lane % 32, i = i0 + 4 * half;
     const int lo = t.lo[i0 + lane % 32], hi = t.hi[i0 + lane % 32];
     if (__ballot(lo < k0 + 32 && hi > k0) == 0) return;
     // Rows that see nothing have no statistics: they are masked, not taken for full.
     const bool mask = __ballot(lo <= k0 && hi >= k0 + 32) != ~0ull;
+    const bool both_sides = rule.sloped && __ballot(t.at[i0 + lane % 32] != INFINITY) != 0;
     qt += i0 * ld;
     gt += i0 * ld;
-    f32x16 s(0.0f), dp(0.0f);
+    f32x16 s(0.0f), dp;  // dp: the products less delta
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const f32x4 less = four_at<f32x4>(&t.less[i + 2 * r]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[r + e] = less[e];
+    }
     {
       frag<T> x[DP / 16];
 #pragma unroll
@@ -1111,35 +1171,14 @@ template <class T, int DP> struct BackwardK {
 #pragma unroll
       for (int c = 0; c < DP / 16; ++c) dp = mma(x[c], v[c], dp);
     }
-    const int i = i0 + 4 * half;
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const f32x4 delta = four_at<f32x4>(&t.delta[i + 2 * r]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) dp[r + e] -= delta[e];
-    }
     if (rule.capped) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
-        dp[r] *= fmaf(-s[r], s[r], 1.0f);
+        s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
+        dp[r] *= bend_of<T>(s[r]);
       }
     }
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const f32x4 lse = four_at<f32x4>(&t.lse[i + 2 * r]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, -lse[e]);
-    }
-    if (rule.sloped) {
-      const float place = (float)key;
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const f32x4 slope = four_at<f32x4>(&t.slope[i + 2 * r]), at = four_at<f32x4>(&t.at[i + 2 * r]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[r + e] = fmaf(-slope[e], fabsf(at[e] - place), s[r + e]);
-      }
-    }
+    t.add_to(s, i, key - kb0, both_sides, rule);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       s[r] = __builtin_amdgcn_exp2f(s[r]);
@@ -1198,7 +1237,7 @@ __device__ __forceinline__ Interval rows_seeing(const AttnParams& p, int b, int 
 template <class T, int DP> __device__ __forceinline__ void store_keys(const AttnParams& p, int b, int hk, int key, const f32x16* dk, const f32x16* dv, int lane) {
   if (key >= p.Tk) return;
   store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, dk, p.scale, lane / 32, p.D, p.vec);
-  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, 1.0f, lane / 32, p.D, p.vec);
+  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, p_unit<T>(p), lane / 32, p.D, p.vec);
 }
 
 // Few rows or keys, and all keys in fp32: 32 of them a workgroup, whose four waves take
@@ -1219,9 +1258,9 @@ template <class T, int DP, bool KEEP> __device__ __forceinline__ void few_rows(c
   const int tile = p.causal ? tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, lds.range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   BackwardQ<T, DP> f;
-  start_dq<T, DP, KEEP>(p, f, w, at.pair, b, hk, lane, wave == 0);
+  start_dq<T, DP, KEEP>(p, f, w, rule, at.pair, b, hk, lane, wave == 0);
   Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
   int k0 = keys.lo / 32 * 32 + 32 * wave;
   if (k0 < keys.hi) {
@@ -1254,7 +1293,7 @@ template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(co
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const int k0 = 32 * at.tile, key = k0 + lane % 32;
   const Interval rows = rows_seeing<OWN>(p, b, tq, k0, 32, tk, lds.range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
   Stage<T, DP, 32, 64, true> qs(p, p.q, b, hk, tq * p.G, lane), gs(p, p.dout, b, hk, tq * p.G, lane);
@@ -1282,7 +1321,7 @@ template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(co
       gs.store(lds.b[wave], LD);
       learn(r0);
     }
-    if (lane < 32) lds.table[wave].put(lane, info, tk - tq, rows.hi);
+    if (lane < 32) lds.table[wave].put(lane, info, tk - tq, rows.hi, rule, k0, 32);
     wave_sync();
     const int next = r0 + 32 * kWaves;
     if (kAhead && next < rows.hi) {
@@ -1290,7 +1329,7 @@ template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(co
       gs.load(next);
       learn(next);
     }
-    f.step(lds.a[wave], lds.b[wave], LD, lds.table[wave], 0, k0, rule, lane);
+    f.step(lds.a[wave], lds.b[wave], LD, lds.table[wave], 0, k0, k0, rule, lane);
     wave_sync();
   }
   add_waves<kWaves>(f.dk, reinterpret_cast<float*>(lds.a), wave, lane);
@@ -1343,7 +1382,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
   const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   Stage<T, DP, RT, kThreads, true> qs(p, p.q, b, hk, tq * p.G, tid), gs(p, p.dout, b, hk, tq * p.G, tid);
   RowInfo info;
   const int first = rows.lo / 32 * 32;
@@ -1355,7 +1394,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   const auto put = [&](int to) {
     qs.store(tiles[to][0], LD);
     gs.store(tiles[to][1], LD);
-    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi);
+    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi, rule, kb0, 64);
   };
   if (first < rows.hi) {
     fetch(first);
@@ -1366,7 +1405,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   for (int r0 = first; r0 < rows.hi; r0 += RT, cur ^= 1) {
     const bool more = r0 + RT < rows.hi;
     if (more) fetch(r0 + RT);
-    f.step(tiles[cur][0], tiles[cur][1], LD, table[cur], 32 * by_row, k0, rule, lane);
+    f.step(tiles[cur][0], tiles[cur][1], LD, table[cur], 32 * by_row, kb0, k0, rule, lane);
     if (more) put(cur ^ 1);
     __syncthreads();
   }
@@ -1408,7 +1447,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
     for (int c = 0; c < DP / 16; ++c) own[c] = key < tk ? load_frag(row, 16 * c + 8 * half, p.D, p.vec) : frag<T>(0);
   }
   const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
-  const ScoreRule rule = score_rule(p);
+  const ScoreRule rule = score_rule<T>(p);
   // The first kind brings the queries, the second the gradients.
   const HeadView brings = scores ? p.q : p.dout;
   Stage<T, DP, RT, kThreads, true> st(p, brings, b, hk, tq * p.G, tid % kThreads);
@@ -1423,7 +1462,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
   };
   const auto put = [&](int to) {
     st.store(tiles[to][scores ? 0 : 1], LD);
-    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi);
+    if (tid < RT) table[to].put(tid, info, tk - tq, rows.hi, rule, kb0, 64);
   };
   if (n > 0) {
     fetch(0);
@@ -1443,6 +1482,14 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
       f32x4(&pr)[4][64] = probs[(scores ? t : t - 1) & 1][block];
       const T* rt = tiles[mine][scores ? 0 : 1] + i0 * LD;
       f32x16 s(0.0f);
+      if (!scores) {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 less = four_at<f32x4>(&tab.less[i + 2 * r]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[r + e] = less[e];
+        }
+      }
       {
         frag<T> x[DP / 16];
 #pragma unroll
@@ -1455,25 +1502,11 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
         if (rule.capped) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = tanh_of<T>(s[r], rule.pre, rule.twice_pre);
-            bend[r] = fmaf(-s[r], s[r], 1.0f);
+            s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
+            bend[r] = bend_of<T>(s[r]);
           }
         }
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const f32x4 lse = four_at<f32x4>(&tab.lse[i + 2 * r]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[r + e] = fmaf(s[r + e], rule.mul, -lse[e]);
-        }
-        if (rule.sloped) {
-          const float place = (float)key;
-#pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            const f32x4 slope = four_at<f32x4>(&tab.slope[i + 2 * r]), where = four_at<f32x4>(&tab.at[i + 2 * r]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[r + e] = fmaf(-slope[e], fabsf(where[e] - place), s[r + e]);
-          }
-        }
+        tab.add_to(s, i, key - kb0, rule.sloped && __ballot(tab.at[i0 + lane % 32] != INFINITY) != 0, rule);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
         // Rows that see nothing have no statistics: they are masked, not taken for full.
@@ -1493,20 +1526,30 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
       } else {
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-          const f32x4 delta = four_at<f32x4>(&tab.delta[i + 2 * r]), x = pr[r / 4][lane];
+          const f32x4 x = pr[r / 4][lane];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[r + e] = x[e] * (s[r + e] - delta[e]);
+          for (int e = 0; e < 4; ++e) s[r + e] *= x[e];
         }
+      }
+      // p in one part, ds in two.
+      frag<T> hi[2], lo[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) hi[h] = lo[h] = acc_frag<T>(s, h);
+      if (!scores) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) lo[h] = Parts<T>(s, h).lo;
       }
       const T* ct = tiles[mine][scores ? 1 : 0] + i0 * LD;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Parts<T> f(s, h);
+        frag<T> x[DP / 32];
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
-          const frag<T> x = cols_frag(ct, LD, h, 32 * d, lane);
-          sum[d] = mma(x, f.hi, sum[d]);
-          if (Parts<T>::kTwo && !scores) sum[d] = mma(x, f.lo, sum[d]);
+        for (int d = 0; d < DP / 32; ++d) x[d] = cols_frag(ct, LD, h, 32 * d, lane);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) sum[d] = mma(x[d], hi[h], sum[d]);
+        if (!scores) {
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) sum[d] = mma(x[d], lo[h], sum[d]);
         }
       }
     }
@@ -1517,7 +1560,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
   add_waves<2>(sum, reinterpret_cast<float*>(tiles) + (wave / 4 * 2 + by_key) * ((DP / 32) * 16 * 64), by_row, lane);
   if (by_row != 0 || key >= p.Tk) return;
   if (scores)
-    store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, sum, 1.0f, half, p.D, p.vec);
+    store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, sum, p_unit<T>(p), half, p.D, p.vec);
   else
     store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, sum, p.scale, half, p.D, p.vec);
 }
