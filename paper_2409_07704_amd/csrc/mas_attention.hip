@@ -30,11 +30,11 @@
 //     exponents and sums, two waves a SIMD (8 items of 4096 causal frames, 16 heads of
 //     128 over 4, bf16: 643 us, 855 TFLOP/s);
 //   gradients: the vector pipe beside them (4 items, 8 heads over 2, capped, sloped:
-//     dq 338 us for 3 products of 34 GFLOP and their recomputed exponents, dk and dv
-//     570 us for 4; forward 263);
+//     dq 325 us for 3 products of 34 GFLOP and their recomputed exponents, dk and dv
+//     527 us for 4; forward 251);
 //   short passes and documents: the chain of dependent steps from lengths to tables to
 //     tiles, about 1 us each, and few tiles behind it (64 items of up to 1001 tokens, 3
-//     heads of 64, 5 documents: 42 + 53 + 86 us for 173 MB);
+//     heads of 64, 5 documents: 43 + 55 + 87 us for 173 MB);
 //   steps over caches: memory (64 caches of up to 4096 keys, 203 MB: 43 us, 4.7 TB/s,
 //     and 5 us to join the parts).
 #include <hip/hip_runtime.h>
