@@ -272,7 +272,8 @@ typedef enum mas_dtype { MAS_F32 = 0, MAS_F16 = 1, MAS_BF16 = 2 } mas_dtype;
  * a head (any values whose addresses stay in the tensor; 0 repeats an input);
  * the D channels of a head are contiguous.  16-byte accesses are used where
  * every head of every tensor of the call starts on a 16-byte boundary and D
- * elements are whole 16-byte pieces; else element accesses (slower).
+ * elements are whole 16-byte pieces; else element accesses (slower).  Strides
+ * of a token or a head that go backwards take the slower way as well.
  */
 typedef struct mas_heads {
   void* data;

@@ -261,7 +261,9 @@ template <class T, int DP, int ROWS, int TEAM, bool BY_ROWS> struct Stage {
   __device__ __forceinline__ Stage(const AttnParams& p, const HeadView& v, int b, int hk, int limit, int tid)
       : p(p), v(v), base(head<T>(v, b, BY_ROWS ? hk * p.G : hk)), tid(tid), limit(limit), whole(false), at(0) {
     const int most = (1 << 29) / (ROWS * (int)sizeof(T));
-    fast = p.vec && v.st < most && (!BY_ROWS || (32 % p.G == 0 && v.sh < most));
+    // Offsets inside a tile are unsigned 32-bit numbers: strides that go backwards, which
+    // they do not hold, take the element-by-element way.
+    fast = p.vec && v.st >= 0 && v.st < most && (!BY_ROWS || (32 % p.G == 0 && v.sh >= 0 && v.sh < most));
 #pragma unroll
     for (int n = 0; n < (kEven ? 1 : N); ++n) {
       const int i = row(n), c = col(n) < p.D ? col(n) : 0;
