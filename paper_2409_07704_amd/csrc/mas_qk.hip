@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(kThreads) mas_qk_any_backward_kernel(const QkP
 #pragma unroll
       for (int j = 0; j < kAny; ++j) {
         const int c = lane + 64 * j;
-        x[j] *= r;
+        x[j] = s.used && c < p.D ? x[j] * r : 0.0f;  // r is infinite for zeros without eps
         if (h < p.Hq)
           dwq[j] += g[j] * x[j];
         else
