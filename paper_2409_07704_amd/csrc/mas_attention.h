@@ -41,7 +41,7 @@ struct AttnPlan {
   int32_t waves;  // else: of 32 rows each in a workgroup
   int32_t tiles, splits, span;
 };
-AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32);
+AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32, float cap);
 size_t attention_part_bytes(const AttnPlan& plan, int32_t pairs, int32_t D);
 
 hipError_t launch_attention(AttnParams p, int dtype, const AttnPlan& plan, hipStream_t stream);

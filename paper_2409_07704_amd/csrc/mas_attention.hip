@@ -65,6 +65,7 @@ constexpr int kMaxWaves = 8;
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.0f;  // powers of two
+constexpr float kHalfCap = 256.0f;
 
 // Eight elements of an operand: one lane's share of 16 steps of a contraction.
 template <class T> struct Frag;
@@ -110,15 +111,20 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // A capped score by way of r = -1 / (e^2x + 1): tanh(x) = 1 + 2 r, whose last step the
-// next factor takes along, and tanh'(x) = -4 (r + r r).  The absolute error of about 2^-23
-// in tanh is not enough next to x itself in fp32 with |x| < 1/4: there the Taylor sum up
-// to x^9, whose next term is below 2^-26 of x, and in fp32 tanh itself in r's place.  x is
-// a product times `pre`; twice_pre: 2 pre in powers of two.
-template <class T> constexpr bool kByHalf = sizeof(T) == 2;
-template <class T> __device__ __forceinline__ float bent(float product, float pre, float twice_pre) {
+// next factor takes along, and tanh'(x) = -4 (r + r r).  x is a product times `pre`;
+// twice_pre: 2 pre in powers of two.  tanh so has an absolute error of up to 2.5 units
+// of 2^-23, and a score, cap times it, an error that grows with the cap however small
+// the score is.  Up to kHalfCap in 16-bit types that is a sixth at most of the rounding
+// of p.  Larger caps, and fp32, take tanh itself (EXACT): for |x| < 1/4 the Taylor sum up
+// to x^9, whose next term is below 2^-26 of x, so that a score has a relative error.  In
+// the kernels of the ordinary caps that way spilled registers (dq of 128 channels 5 of
+// them, of 64 channels 33), so large caps in 16 bits have kernels of their own, those of
+// few rows and keys (4 x 4096 causal frames of 8 heads of 128, bf16, cap 50 / 257: 247 /
+// 661 us, gradients 861 / 1587).
+template <bool EXACT> __device__ __forceinline__ float bent(float product, float pre, float twice_pre) {
   const float e = __builtin_amdgcn_exp2f(product * twice_pre);
   const float r = __builtin_amdgcn_rcpf(-1.0f - e);
-  if constexpr (!kByHalf<T>) {
+  if constexpr (EXACT) {
     const float t = fmaf(2.0f, r, 1.0f);
     const float x = product * pre, y = x * x;
     float s = fmaf(y, 62.0f / 2835.0f, -17.0f / 315.0f);
@@ -129,8 +135,10 @@ template <class T> __device__ __forceinline__ float bent(float product, float pr
   }
   return r;
 }
+// The way of ordinary caps.
+template <class T> constexpr bool kExact = sizeof(T) == 4;
 // tanh', without its factor 4 where r stands for tanh.
-template <class T> __device__ __forceinline__ float bend_of(float x) { return fmaf(-x, x, kByHalf<T> ? -x : 1.0f); }
+template <bool EXACT> __device__ __forceinline__ float bend_of(float x) { return fmaf(-x, x, EXACT ? 1.0f : -x); }
 
 // 1 / l, and 0 where nothing was summed; NaN stays.
 __device__ __forceinline__ float inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -450,21 +458,22 @@ __device__ __forceinline__ Seen seen(int lo, int hi, int k, int n) {
 // That is mul x + add of the product, or of what `bent` makes of it, and the forward
 // pass brings `add` in with the log-sum-exp.  lift: added to the exponent where tanh'
 // lacks its factor 4, so that ds has it (and p, until dv is stored).
-struct ScoreRule {
+template <bool EXACT> struct ScoreRule {
+  static constexpr bool kExactly = EXACT;
   float pre, twice_pre, mul, add, lift;
   bool capped, sloped;
 };
-template <class T> __device__ __forceinline__ float score_add(const AttnParams& p) { return kByHalf<T> && p.cap > 0.0f ? p.cap * kLog2E : 0.0f; }
-template <class T> __device__ __forceinline__ ScoreRule score_rule(const AttnParams& p) {
-  ScoreRule s;
+template <bool EXACT> __device__ __forceinline__ float score_add(const AttnParams& p) { return !EXACT && p.cap > 0.0f ? p.cap * kLog2E : 0.0f; }
+template <bool EXACT> __device__ __forceinline__ ScoreRule<EXACT> score_rule(const AttnParams& p) {
+  ScoreRule<EXACT> s;
   s.capped = p.cap > 0.0f;
   s.sloped = p.slope != nullptr;
   s.pre = s.capped ? p.scale / p.cap : 1.0f;
   s.twice_pre = s.pre * (2.0f * kLog2E);
   s.mul = (s.capped ? p.cap : p.scale) * kLog2E;
-  s.add = score_add<T>(p);
+  s.add = score_add<EXACT>(p);
   s.lift = 0.0f;
-  if (kByHalf<T> && s.capped) {
+  if (!EXACT && s.capped) {
     s.mul *= 2.0f;
     s.lift = 2.0f;
   }
@@ -472,7 +481,7 @@ template <class T> __device__ __forceinline__ ScoreRule score_rule(const AttnPar
 }
 
 // What undoes `lift`.
-template <class T> __device__ __forceinline__ float p_unit(const AttnParams& p) { return kByHalf<T> && p.cap > 0.0f ? 0.25f : 1.0f; }
+template <bool EXACT> __device__ __forceinline__ float p_unit(const AttnParams& p) { return !EXACT && p.cap > 0.0f ? 0.25f : 1.0f; }
 
 // ------------------------------------------------------------------ forward
 // Keys of a tile: 64, or 32 in fp32, whose rows are twice as long.
@@ -495,7 +504,7 @@ template <class T, int DP> struct Forward {
     l = 0.0f;
   }
   // NB blocks of 32 keys from k0 on, in LDS.
-  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int ldv, int k0, const Rows& w, const ScoreRule& rule, int lane) {
+  template <int NB, class Rule> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int ldv, int k0, const Rows& w, const Rule& rule, int lane) {
     const Seen how = seen(w.lo, w.hi, k0, 32 * NB);
     if (how == Seen::none) return;
     const int half = lane / 32;
@@ -514,7 +523,7 @@ template <class T, int DP> struct Forward {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = bent<T>(s[n][r], rule.pre, rule.twice_pre);
+        for (int r = 0; r < 16; ++r) s[n][r] = bent<Rule::kExactly>(s[n][r], rule.pre, rule.twice_pre);
     }
     if (general) {
 #pragma unroll
@@ -585,12 +594,12 @@ template <class T, int DP> __device__ __forceinline__ void load_q(const AttnPara
 
 // The rows of one wave over the keys [from, to); with `part` sums, maximum and
 // total go there, at this lane's row.
-template <class T>
+template <class T, bool EXACT>
 __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, int b, int hk, int from, int to, float* part) {
   const int lane = threadIdx.x % 64, half = lane / 32;
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const Rows w = rows_of(p, row, b, hk, tq, tk);
-  const ScoreRule rule = score_rule<T>(p);
+  const ScoreRule<EXACT> rule = score_rule<EXACT>(p);
   const T* qr = head<T>(p.q, b, w.h) + (int64_t)w.tok * p.q.st;
   const T* kb = head<T>(p.k, b, hk);
   const T* vb = head<T>(p.v, b, hk);
@@ -617,7 +626,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
       for (int r = 0; r < 16; ++r) {
         const int at = k0 + acc_row(r, half);
         const bool sees = (at >= w.lo) & (at < w.hi);
-        float x = rule.capped ? bent<T>(s[r], rule.pre, rule.twice_pre) : s[r];
+        float x = rule.capped ? bent<EXACT>(s[r], rule.pre, rule.twice_pre) : s[r];
         x = fmaf(-w.slope, fabsf((float)(w.at - at)), x * rule.mul);
         s[r] = sees ? x : -INFINITY;
         top = fmaxf(top, s[r]);
@@ -675,7 +684,7 @@ __device__ __forceinline__ void forward_carefully(const AttnParams& p, int row, 
     part[p.D] = m;
     part[p.D + 1] = l;
   } else if (p.lse) {
-    p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (m + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
+    p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (m + __builtin_amdgcn_logf(l) + score_add<EXACT>(p)) * kLn2;
   }
 }
 
@@ -706,7 +715,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 3 : 2) ma
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<kExact<T>>(p);
 
   Forward<T, DP> f;
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
@@ -736,18 +745,18 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 3 : 2) ma
     __syncthreads();
   }
   if (__ballot(w.hi > w.lo && !finite(f.o)) != 0)
-    return forward_carefully<T>(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, keys.lo, keys.hi, nullptr);
+    return forward_carefully<T, kExact<T>>(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, keys.lo, keys.hi, nullptr);
   if (!w.in) return;
   if (w.hi <= w.lo) f.clear();
   const float l = add_halves(f.l);
   store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
-  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (f.m + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (f.m + __builtin_amdgcn_logf(l) + score_add<kExact<T>>(p)) * kLn2;
 }
 
 // Few rows: 32 a workgroup, whose four waves take the blocks of 32 keys in turn,
 // each with its own maximum, total and sums, joined at the end; with `splits` > 1
 // a workgroup takes a part of the keys and a second kernel joins the parts.
-template <class T, int DP>
+template <class T, int DP, bool EXACT>
 __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnParams p) {
   constexpr int LD = kLd<T, DP>, LDV = kLdCols<T, DP>;
   struct Tiles {
@@ -769,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
   Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<EXACT>(p);
   keys.lo = max(keys.lo / 32 * 32, at.split * p.span);
   keys.hi = min(keys.hi, (at.split + 1) * p.span);
 
@@ -799,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
   float* part = p.part + (((size_t)at.split * p.pairs + at.pair) * (32 * (size_t)p.tiles) + w.row) * (p.D + 2);
   // Also the barrier between the tiles and the sums, which share LDS.
   if (__syncthreads_or(w.hi > w.lo && !finite(f.o))) {
-    if (wave == 0) forward_carefully<T>(p, 32 * tile + lane % 32, b, hk, keys.lo, keys.hi, p.splits > 1 ? part : nullptr);
+    if (wave == 0) forward_carefully<T, EXACT>(p, 32 * tile + lane % 32, b, hk, keys.lo, keys.hi, p.splits > 1 ? part : nullptr);
     return;
   }
   if (wave > 0) {
@@ -844,11 +853,11 @@ __global__ void __launch_bounds__(kThreads, 1) mas_attention_keys(const AttnPara
     return;
   }
   store_row<T, DP>(head_out<T>(p.out, b, w.h) + (int64_t)w.tok * p.out.st, f.o, inverse(l), lane / 32, p.D, p.vec);
-  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (top + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
+  if (p.lse && lane < 32) p.lse[((size_t)b * p.Hq + w.h) * p.Tq + w.tok] = (top + __builtin_amdgcn_logf(l) + score_add<EXACT>(p)) * kLn2;
 }
 
 // The parts of a row, joined: a wave for each row, two channels a lane.
-template <class T>
+template <class T, bool EXACT>
 __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams p) {
   const size_t n = (size_t)blockIdx.x * kWaves + threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
@@ -897,7 +906,7 @@ __global__ void __launch_bounds__(kThreads) mas_attention_join(const AttnParams 
 #pragma unroll
   for (int e = 0; e < 2; ++e)
     if (lane + 64 * e < p.D) out[lane + 64 * e] = (T)(mul != 0.0f ? x[e] * mul : 0.0f);
-  if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.Tq + tok] = (top + __builtin_amdgcn_logf(l) + score_add<T>(p)) * kLn2;
+  if (p.lse && lane == 0) p.lse[((size_t)b * p.Hq + h) * p.Tq + tok] = (top + __builtin_amdgcn_logf(l) + score_add<EXACT>(p)) * kLn2;
 }
 
 // ----------------------------------------------------------------- backward
@@ -928,7 +937,7 @@ template <class T, int DP> struct BackwardQ {
   frag<T> q[DP / 16], g[DP / 16];  // queries and gradients of the output
   f32x16 dq[DP / 32];
   float base, delta;  // base: what the exponent has besides the score's factor
-  template <int NB> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const ScoreRule& rule, int lane) {
+  template <int NB, class Rule> __device__ __forceinline__ void step(const T* kt, const T* vt, int ld, int k0, const Rows& w, const Rule& rule, int lane) {
     const int half = lane / 32;
 #pragma unroll
     for (int n = 0; n < NB; ++n, kt += 32 * ld, vt += 32 * ld, k0 += 32) {
@@ -944,8 +953,8 @@ template <class T, int DP> struct BackwardQ {
       if (rule.capped) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
-          dp[r] *= bend_of<T>(s[r]);
+          s[r] = bent<Rule::kExactly>(s[r], rule.pre, rule.twice_pre);
+          dp[r] *= bend_of<Rule::kExactly>(s[r]);
         }
       }
 #pragma unroll
@@ -977,8 +986,8 @@ template <class T, int DP> struct BackwardQ {
 
 // What a wave's rows need before their keys: queries, gradients, statistics.  KEEP:
 // the kernel of dk and dv will want them.
-template <class T, int DP, bool KEEP>
-__device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& f, const Rows& w, const ScoreRule& rule, int pair, int b, int hk, int lane, bool first) {
+template <class T, int DP, bool KEEP, class Rule>
+__device__ __forceinline__ void start_dq(const AttnParams& p, BackwardQ<T, DP>& f, const Rows& w, const Rule& rule, int pair, int b, int hk, int lane, bool first) {
   load_q<T, DP>(p, p.q, w, b, lane, f.q);
   load_q<T, DP>(p, p.dout, w, b, lane, f.g);
   f.delta = 0.0f;
@@ -1018,7 +1027,7 @@ __global__ void __launch_bounds__(64 * W, sizeof(T) == 4 ? 1 : DP <= 64 ? 3 : 2)
   const int tile = p.causal ? p.tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * W * tile + 32 * wave + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<kExact<T>>(p);
   BackwardQ<T, DP> f;
   start_dq<T, DP, true>(p, f, w, rule, at.pair, b, hk, lane, true);
   const int first = keys.lo / KT * KT;
@@ -1088,7 +1097,7 @@ template <int ROWS> struct RowTable {
   float base[ROWS], less[ROWS], slope[ROWS], at[ROWS];  // less: -delta
   int lo[ROWS], hi[ROWS];
   // shift: from a token to its place; rows from `limit` on see nothing.
-  __device__ __forceinline__ void put(int i, const RowInfo& x, int shift, int limit, const ScoreRule& rule, int kb0, int keys) {
+  template <class Rule> __device__ __forceinline__ void put(int i, const RowInfo& x, int shift, int limit, const Rule& rule, int kb0, int keys) {
     const int place = x.tok + shift, e = place - kb0;
     const float k = (e > 0 ? x.slope : -x.slope) * kLog2E;
     base[i] = fmaf(-k, (float)e, rule.add + rule.lift - x.stat.x);
@@ -1099,10 +1108,10 @@ template <int ROWS> struct RowTable {
     hi[i] = x.row < limit ? x.see.y : 0;
   }
   // Scores of rows i + 8 n + 0 ... 3 down the registers and the key kb0 + k, complete.
-  __device__ __forceinline__ void add_to(f32x16& s, int i, int k, bool both_sides, const ScoreRule& rule) const;
+  template <class Rule> __device__ __forceinline__ void add_to(f32x16& s, int i, int k, bool both_sides, const Rule& rule) const;
 };
 template <class V> __device__ __forceinline__ V four_at(const void* at) { return *reinterpret_cast<const V*>(at); }
-template <int ROWS> __device__ __forceinline__ void RowTable<ROWS>::add_to(f32x16& s, int i, int k, bool both_sides, const ScoreRule& rule) const {
+template <int ROWS> template <class Rule> __device__ __forceinline__ void RowTable<ROWS>::add_to(f32x16& s, int i, int k, bool both_sides, const Rule& rule) const {
   if (!rule.sloped) {
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
@@ -1146,7 +1155,7 @@ template <class T, int DP> struct BackwardK {
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16(0.0f);
   }
   // Rows i0 ... i0 + 31 of a tile in LDS against the keys from k0 on.
-  template <int ROWS> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int kb0, int k0, const ScoreRule& rule, int lane) {
+  template <int ROWS, class Rule> __device__ __forceinline__ void step(const T* qt, const T* gt, int ld, const RowTable<ROWS>& t, int i0, int kb0, int k0, const Rule& rule, int lane) {
     const int half = lane / 32, key = k0 + lane % 32, i = i0 + 4 * half;
     const int lo = t.lo[i0 + lane % 32], hi = t.hi[i0 + lane % 32];
     if (__ballot(lo < k0 + 32 && hi > k0) == 0) return;
@@ -1176,8 +1185,8 @@ template <class T, int DP> struct BackwardK {
     if (rule.capped) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
-        dp[r] *= bend_of<T>(s[r]);
+        s[r] = bent<Rule::kExactly>(s[r], rule.pre, rule.twice_pre);
+        dp[r] *= bend_of<Rule::kExactly>(s[r]);
       }
     }
     t.add_to(s, i, key - kb0, both_sides, rule);
@@ -1236,10 +1245,10 @@ __device__ __forceinline__ Interval rows_seeing(const AttnParams& p, int b, int 
   return rows;
 }
 
-template <class T, int DP> __device__ __forceinline__ void store_keys(const AttnParams& p, int b, int hk, int key, const f32x16* dk, const f32x16* dv, int lane) {
+template <class T, int DP, bool EXACT> __device__ __forceinline__ void store_keys(const AttnParams& p, int b, int hk, int key, const f32x16* dk, const f32x16* dv, int lane) {
   if (key >= p.Tk) return;
   store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, dk, p.scale, lane / 32, p.D, p.vec);
-  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, p_unit<T>(p), lane / 32, p.D, p.vec);
+  store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, dv, p_unit<EXACT>(p), lane / 32, p.D, p.vec);
 }
 
 // Few rows or keys, and all keys in fp32: 32 of them a workgroup, whose four waves take
@@ -1252,7 +1261,7 @@ template <class T, int DP> struct FewLds {
   static_assert(sizeof(T) * 32 * LD * kWaves >= kWaves / 2 * (DP / 32) * 16 * 64 * sizeof(float), "the waves' sums fit");
 };
 
-template <class T, int DP, bool KEEP> __device__ __forceinline__ void few_rows(const AttnParams& p, const Place& at, int tiles, FewLds<T, DP>& lds) {
+template <class T, int DP, bool KEEP, bool EXACT> __device__ __forceinline__ void few_rows(const AttnParams& p, const Place& at, int tiles, FewLds<T, DP>& lds) {
   constexpr int LD = kLd<T, DP>;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -1260,7 +1269,7 @@ template <class T, int DP, bool KEEP> __device__ __forceinline__ void few_rows(c
   const int tile = p.causal ? tiles - 1 - at.tile : at.tile;
   const Rows w = rows_of(p, 32 * tile + lane % 32, b, hk, tq, tk);
   const Interval keys = key_range(w.lo, w.hi, lds.range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<EXACT>(p);
   BackwardQ<T, DP> f;
   start_dq<T, DP, KEEP>(p, f, w, rule, at.pair, b, hk, lane, wave == 0);
   Stage<T, DP, 32, 64, false> ks(p, p.k, b, hk, tk, lane), vs(p, p.v, b, hk, tk, lane);
@@ -1285,7 +1294,7 @@ template <class T, int DP, bool KEEP> __device__ __forceinline__ void few_rows(c
 }
 
 // OWN: without the statistics and intervals of another kernel.
-template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(const AttnParams& p, const Place& at, FewLds<T, DP>& lds) {
+template <class T, int DP, bool OWN, bool EXACT> __device__ __forceinline__ void few_keys(const AttnParams& p, const Place& at, FewLds<T, DP>& lds) {
   constexpr int LD = kLd<T, DP>;
   // Products take so long in fp32 that the next tile need not be fetched meanwhile,
   // for which there are no registers.
@@ -1295,7 +1304,7 @@ template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(co
   const int tq = clamp_len(p.t_q, b, p.Tq), tk = clamp_len(p.t_k, b, p.Tk);
   const int k0 = 32 * at.tile, key = k0 + lane % 32;
   const Interval rows = rows_seeing<OWN>(p, b, tq, k0, 32, tk, lds.range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<EXACT>(p);
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
   Stage<T, DP, 32, 64, true> qs(p, p.q, b, hk, tq * p.G, lane), gs(p, p.dout, b, hk, tq * p.G, lane);
@@ -1336,19 +1345,19 @@ template <class T, int DP, bool OWN> __device__ __forceinline__ void few_keys(co
   }
   add_waves<kWaves>(f.dk, reinterpret_cast<float*>(lds.a), wave, lane);
   add_waves<kWaves>(f.dv, reinterpret_cast<float*>(lds.a), wave, lane);
-  if (wave == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
+  if (wave == 0) store_keys<T, DP, EXACT>(p, b, hk, key, f.dk, f.dv, lane);
 }
 
-template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dq_few(const AttnParams p) {
+template <class T, int DP, bool EXACT> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dq_few(const AttnParams p) {
   __shared__ __align__(16) FewLds<T, DP> lds;
   const Place at = place_of(p);
-  if (!at.idle) few_rows<T, DP, true>(p, at, p.tiles, lds);
+  if (!at.idle) few_rows<T, DP, true, EXACT>(p, at, p.tiles, lds);
 }
 
-template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
+template <class T, int DP, bool EXACT> __global__ void __launch_bounds__(kThreads, 1) mas_attention_dkv(const AttnParams p) {
   __shared__ __align__(16) FewLds<T, DP> lds;
   const Place at = place_of(p);
-  if (!at.idle) few_keys<T, DP, false>(p, at, lds);
+  if (!at.idle) few_keys<T, DP, false, EXACT>(p, at, lds);
 }
 
 // Both at once, the first `split` workgroups for dq, where neither fills the chip.
@@ -1358,9 +1367,9 @@ template <class T, int DP> __global__ void __launch_bounds__(kThreads, 1) mas_at
   const Place at = place_of(p, by_rows ? blockIdx.x : blockIdx.x - split, by_rows ? row_tiles : key_tiles);
   if (at.idle) return;
   if (by_rows)
-    few_rows<T, DP, false>(p, at, row_tiles, lds);
+    few_rows<T, DP, false, kExact<T>>(p, at, row_tiles, lds);
   else
-    few_keys<T, DP, true>(p, at, lds);
+    few_keys<T, DP, true, kExact<T>>(p, at, lds);
 }
 
 // 16-bit types: 64 keys a workgroup, two waves by keys and two by rows, which
@@ -1384,7 +1393,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   BackwardK<T, DP> f;
   f.start(p, b, hk, key, tk, lane);
   const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<kExact<T>>(p);
   Stage<T, DP, RT, kThreads, true> qs(p, p.q, b, hk, tq * p.G, tid), gs(p, p.dout, b, hk, tq * p.G, tid);
   RowInfo info;
   const int first = rows.lo / 32 * 32;
@@ -1414,7 +1423,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) mas_attention_dkv_
   float* sums = reinterpret_cast<float*>(tiles) + by_key * ((DP / 32) * 16 * 64);
   add_waves<2>(f.dk, sums, by_row, lane);
   add_waves<2>(f.dv, sums, by_row, lane);
-  if (by_row == 0) store_keys<T, DP>(p, b, hk, key, f.dk, f.dv, lane);
+  if (by_row == 0) store_keys<T, DP, kExact<T>>(p, b, hk, key, f.dk, f.dv, lane);
 }
 
 // The same for more than 64 channels, whose two sums do not fit the registers of
@@ -1449,7 +1458,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
     for (int c = 0; c < DP / 16; ++c) own[c] = key < tk ? load_frag(row, 16 * c + 8 * half, p.D, p.vec) : frag<T>(0);
   }
   const Interval rows = rows_seeing(p, b, tq, kb0, 64, tk, range);
-  const ScoreRule rule = score_rule<T>(p);
+  const auto rule = score_rule<kExact<T>>(p);
   // The first kind brings the queries, the second the gradients.
   const HeadView brings = scores ? p.q : p.dout;
   Stage<T, DP, RT, kThreads, true> st(p, brings, b, hk, tq * p.G, tid % kThreads);
@@ -1504,8 +1513,8 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
         if (rule.capped) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            s[r] = bent<T>(s[r], rule.pre, rule.twice_pre);
-            bend[r] = bend_of<T>(s[r]);
+            s[r] = bent<kExact<T>>(s[r], rule.pre, rule.twice_pre);
+            bend[r] = bend_of<kExact<T>>(s[r]);
           }
         }
         tab.add_to(s, i, key - kb0, rule.sloped && __ballot(tab.at[i0 + lane % 32] != INFINITY) != 0, rule);
@@ -1562,7 +1571,7 @@ __global__ void __launch_bounds__(2 * kThreads, 2) mas_attention_dkv_pairs(const
   add_waves<2>(sum, reinterpret_cast<float*>(tiles) + (wave / 4 * 2 + by_key) * ((DP / 32) * 16 * 64), by_row, lane);
   if (by_row != 0 || key >= p.Tk) return;
   if (scores)
-    store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, sum, p_unit<T>(p), half, p.D, p.vec);
+    store_row<T, DP>(head_out<T>(p.dv, b, hk) + (int64_t)key * p.dv.st, sum, p_unit<kExact<T>>(p), half, p.D, p.vec);
   else
     store_row<T, DP>(head_out<T>(p.dk, b, hk) + (int64_t)key * p.dk.st, sum, p.scale, half, p.D, p.vec);
 }
@@ -1582,6 +1591,18 @@ uint32_t grid_of(AttnParams& p) {
 template <class T, int DP> constexpr bool kWide = sizeof(T) == 2 && DP == 128;
 bool wide_rows(int32_t pairs, int32_t rows) { return (int64_t)((rows + 255) / 256) * pairs >= 256; }
 
+// Caps for which 16-bit types have kernels of their own (see bent).
+template <class T> bool exact_caps(const AttnParams& p) { return sizeof(T) == 2 && p.cap > kHalfCap; }
+
+template <class T, int DP, bool EXACT> hipError_t forward_keys(const AttnParams& p, uint32_t grid, hipStream_t stream) {
+  hipLaunchKernelGGL((mas_attention_keys<T, DP, EXACT>), dim3(grid), dim3(kThreads), 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const uint64_t rows = (uint64_t)p.pairs * p.rows;
+  hipLaunchKernelGGL((mas_attention_join<T, EXACT>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
 template <class T, int DP> hipError_t forward(AttnParams p, const AttnPlan& plan, hipStream_t stream) {
   const uint32_t grid = grid_of(p);
   if (!plan.small) {
@@ -1594,16 +1615,22 @@ template <class T, int DP> hipError_t forward(AttnParams p, const AttnPlan& plan
     hipLaunchKernelGGL((mas_attention_rows<T, DP, 4>), dim3(grid), dim3(256), 0, stream, p);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((mas_attention_keys<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  const uint64_t rows = (uint64_t)p.pairs * p.rows;
-  hipLaunchKernelGGL((mas_attention_join<T>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)), dim3(kThreads), 0, stream, p);
+  return exact_caps<T>(p) ? forward_keys<T, DP, true>(p, grid, stream) : forward_keys<T, DP, kExact<T>>(p, grid, stream);
+}
+
+template <class T, int DP, bool EXACT> hipError_t backward_few(AttnParams p, hipStream_t stream) {
+  p.tiles = (p.rows + 31) / 32;
+  hipLaunchKernelGGL((mas_attention_dq_few<T, DP, EXACT>), dim3(grid_of(p)), dim3(kThreads), 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  p.tiles = (p.Tk + 31) / 32;
+  hipLaunchKernelGGL((mas_attention_dkv<T, DP, EXACT>), dim3(grid_of(p)), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
 template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream) {
   p.splits = 1;
+  if (exact_caps<T>(p)) return backward_few<T, DP, true>(p, stream);
   // 128 rows a workgroup where those fill the 256 compute units, else 32 (1024 keys of
   // 64 channels, bf16, with dk, dv: 128 workgroups 53.4 / 44.4 us, 256 60.5 / 62.8).
   p.tiles = (p.rows + 127) / 128;
@@ -1632,7 +1659,7 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
   if (wide) p.tiles = (p.rows + 255) / 256;
   uint32_t grid = grid_of(p);
   if (few_rows) {
-    hipLaunchKernelGGL((mas_attention_dq_few<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((mas_attention_dq_few<T, DP, kExact<T>>), dim3(grid), dim3(kThreads), 0, stream, p);
   } else if (!wide) {
     hipLaunchKernelGGL((mas_attention_dq<T, DP, 4>), dim3(grid), dim3(256), 0, stream, p);
   } else {
@@ -1653,7 +1680,7 @@ template <class T, int DP> hipError_t backward(AttnParams p, hipStream_t stream)
   }
   p.tiles = (p.Tk + 31) / 32;
   grid = grid_of(p);
-  hipLaunchKernelGGL((mas_attention_dkv<T, DP>), dim3(grid), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((mas_attention_dkv<T, DP, kExact<T>>), dim3(grid), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -1666,7 +1693,7 @@ template <class T, class F> hipError_t by_width(int D, F&& f) {
 
 }  // namespace
 
-AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32) {
+AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool fp32, float cap) {
   AttnPlan a;
   a.waves = 4;
   a.splits = 1;
@@ -1681,6 +1708,11 @@ AttnPlan attention_plan(int32_t pairs, int32_t rows, int32_t Tk, int32_t D, bool
   // 45.2 / 29.2, 256 49.4 / 49.1.  Up to 32 rows always the latter (64 caches of 4096
   // keys, 4 heads: 128 / 43; 512 of 1024 keys 25.7 / 26.1; 2048 of 256 keys 32.3 / 37.6).
   a.small = rows <= 32 || (int64_t)a.tiles * pairs < (fp32 || D <= 64 ? 256 : 128);
+  if (!a.small && !fp32 && cap > kHalfCap) {  // keys in one part: the workspace does not depend on the cap
+    a.small = true;
+    a.tiles = (rows + 31) / 32;
+    return a;
+  }
   if (!a.small) {
     if (!fp32 && D > 96 && wide_rows(pairs, rows)) {
       a.waves = 8;

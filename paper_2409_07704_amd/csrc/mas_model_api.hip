@@ -71,7 +71,10 @@ AttnParams params(const mas_attention_desc& d) {
   p.pairs = d.B * d.Hk;
   p.causal = d.causal != 0;
   p.scale = d.scale;
-  p.cap = d.cap;
+  // Caps past these make pre and mul of the kernels infinite or nothing.  A cap of 1e30
+  // bends only scores whose neighbours in fp32 are 1e16 apart and more, one of 1e-30
+  // leaves scores that are all equal in fp32.
+  p.cap = d.cap > 1e30f ? 0.0f : d.cap > 0.0f && d.cap < 1e-30f ? 1e-30f : d.cap;
   while ((1 << p.g_shift) < p.G) ++p.g_shift;
   if ((1 << p.g_shift) != p.G) p.g_mul = (uint32_t)(4294967296ull / p.G) + 1;
   return p;
@@ -140,7 +143,7 @@ extern "C" {
 size_t mas_attention_workspace_bytes(const mas_attention_desc* desc, int32_t backward) {
   if (check_desc(desc) != MAS_OK) return 0;
   const int32_t pairs = desc->B * desc->Hk;
-  const AttnPlan plan = attention_plan(pairs, desc->Tq * (desc->Hq / desc->Hk), desc->Tk, desc->D, desc->dtype == MAS_F32);
+  const AttnPlan plan = attention_plan(pairs, desc->Tq * (desc->Hq / desc->Hk), desc->Tk, desc->D, desc->dtype == MAS_F32, desc->cap);
   size_t n = attention_part_bytes(plan, pairs, desc->D);
   if (backward && stat_bytes(*desc) > n) n = stat_bytes(*desc);
   return round_up(n > 0 ? n : 1);
@@ -155,7 +158,7 @@ mas_status mas_attention(const mas_attention_desc* desc, const mas_heads* q, con
   for (const mas_heads* h : {q, k, v, out})
     if (!elements_ok(*h, elem_bytes(desc->dtype))) return MAS_ERR_BAD_VALUE;
   AttnParams p = params(*desc);
-  const AttnPlan plan = attention_plan(p.pairs, p.rows, p.Tk, p.D, desc->dtype == MAS_F32);
+  const AttnPlan plan = attention_plan(p.pairs, p.rows, p.Tk, p.D, desc->dtype == MAS_F32, p.cap);
   if (!workspace_ok(workspace, workspace_bytes, attention_part_bytes(plan, p.pairs, p.D))) return MAS_ERR_WORKSPACE;
   p.q = view(q);
   p.k = view(k);
