@@ -297,12 +297,6 @@ __device__ __forceinline__ int pos_row(int wp) { return wp & (kMaxRows - 1); }
 static_assert(kMaxRows <= 1 << 13, "a row fits its field");
 
 struct SweepLds {
-  union {
-    uint8_t ring[kWavesPerBlock][kWaveRegion];
-    struct {
-      uint8_t area[kWalkArea];  // windows from the start, row_start table at the end
-    } walk;
-  } u;
   // Mailbox of sweep wave w, read with one load per chunk (lane k: word k):
   //   kReady:   value tiles of chunks < ready are in w's slots (kNever after
   //             the last tile);
@@ -336,8 +330,24 @@ struct SweepLds {
   int req_e[2][kWave];
   i32x4 req_arg[2];             // base chunk, lowest and highest chunk, last request (1) or not (0)
   int req_posted, req_done;
+  // Last, so that the walk's reads of rows below row 0 stay in the block (kBelowArea).
+  alignas(256) union {
+    uint8_t ring[kWavesPerBlock][kWaveRegion];
+    struct {
+      uint8_t area[kWalkArea];  // windows from the start, row_start table at the end
+    } walk;
+  } u;
 };
 static_assert(sizeof(SweepLds) <= 80 * 1024, "two workgroups per CU");
+// Bytes below the walk area that walk_item may read.  It reads 64 rows down from the row
+// the path is in, at least four bytes each, and, whatever the bytes it walks from are (a
+// wave that gave up a wait leaves them unstaged), ends with the group of four chunks in
+// which the path leaves row 0.  In it a path falls to row 63 * -3 - 33 at most by step
+// masks (each climb out of a wave g leads to row 63 g - 1 and 32 rows on at most), to
+// row -445 by descent bytes (63 rows a chunk, or 63 g - 1 and 255 on); a wave's rows lie
+// 32 entries after the chunk's start at least.  So 4 (32 - 222 - 63) and 32 - 445 - 63.
+constexpr int kBelowArea = 1012;
+static_assert(offsetof(SweepLds, u) >= kBelowArea, "reads below row 0 stay in the block");
 // The walk's row_start table (T + 1 entries, and up to 64 more that
 // flush_records may touch) at the end of the walk area.
 __device__ __forceinline__ int* walk_rs(SweepLds& L, int T) {
@@ -701,7 +711,7 @@ __device__ __forceinline__ float sweep_wave(const KParams& p, SweepLds& L, const
   const int lane = x.lane, w = x.w;
   float t = -0.0f;  // lane 0 keeps -0 for the whole sweep (see cols8)
   char* const Lc = reinterpret_cast<char*>(&L);
-  const uint32_t wbase = (uint32_t)w * kWaveRegion;
+  const uint32_t wbase = (uint32_t)offsetof(SweepLds, u) + (uint32_t)w * kWaveRegion;
   auto bound_ptr = [&](int k) __attribute__((always_inline)) -> float* {
     return reinterpret_cast<float*>(Lc + wbase + (uint32_t)k * kSlotStride + kBoundOff);
   };
@@ -1500,7 +1510,7 @@ __device__ __forceinline__ void walk_item(const KParams& p, SweepLds& L, const W
     return RING ? area + (ch / kBlk % wp.blocks) * wp.bytes + ch % kBlk * stride : area + ch * stride;
   };
   // The entries of the chunk at LDS address `at` for rows eb, ..., eb - 63
-  // (lane k: row eb - k; lanes past row 0 read whatever is there).
+  // (lane k: row eb - k; lanes past row 0 read whatever is there, see kBelowArea).
   const int lane_off = row0 - lane * kEnt;
   auto fetch = [&](int at, int eb) __attribute__((always_inline)) -> uint32_t {
     const uint32_t a = (uint32_t)(at + eb * kEnt + lane_off);
@@ -1729,11 +1739,12 @@ __device__ __forceinline__ void walk(const KParams& p, SweepLds& L, int b, int t
     // The bytes of chunk ch for rows e_b, e_b - 1, ..., e_b - 63 (lane k:
     // row e_b - k; rows are consecutive bytes), read from ch's window into
     // one register.  Lanes past row 0 or the window read whatever is there,
-    // never used.
-    const uint32_t lane_off = (uint32_t)(-lane);
+    // never used; a place outside the block (only once a wait was given up, when
+    // rows and windows need not fit each other) becomes its nearest byte.
+    auto in_block = [](int at) __attribute__((always_inline)) -> uint32_t { return (uint32_t)min(max(at, 0), (int)sizeof(SweepLds) - 1); };
     auto fetch = [&](int ch, int e_b) __attribute__((always_inline)) -> uint32_t {
-      const uint32_t base = (uint32_t)__builtin_amdgcn_readlane((int)bases, ch & (kWave - 1));
-      return *(const lds_u8*)(uintptr_t)(base + (uint32_t)e_b + lane_off);
+      const int base = __builtin_amdgcn_readlane((int)bases, ch & (kWave - 1));
+      return *(const lds_u8*)(uintptr_t)in_block(base + e_b - lane);
     };
     // One chunk: its byte from lane bp - e of P (P holds the chunk's bytes
     // from row bp down), then P refilled with chunk cw - 2 from row e, the
@@ -1750,8 +1761,8 @@ __device__ __forceinline__ void walk(const KParams& p, SweepLds& L, int b, int t
         const uint32_t pos = d - kEscape;
         s = e - kRowsPerWave * g + 1;
         if (pos < kChunk - 1) {
-          const uint32_t mb = (uint32_t)__builtin_amdgcn_readlane((int)mids, cw & (kWave - 1));
-          s += uni((int)*(const lds_u8*)(uintptr_t)(mb + (uint32_t)(kChunk * (g - 1)) + pos + 1));
+          const int mb = __builtin_amdgcn_readlane((int)mids, cw & (kWave - 1));
+          s += uni((int)*(const lds_u8*)(uintptr_t)in_block(mb + kChunk * (g - 1) + (int)pos + 1));
         }
         g -= 1;
       }
@@ -2224,7 +2235,7 @@ __global__ void __launch_bounds__(kThreads, 4) mas_kernel(KParams p) {
                            ? (ty - 1) / (kChunk * kBlk)
                            : walk_pos((ty + kChunk - 1) / kChunk, max(tx - 1, 0)));
   }
-  if (threadIdx.x < kWave) L.wbase[threadIdx.x] = (int)lds_off(&L.u.walk.area[0]);
+  if (threadIdx.x < kWave) L.wbase[threadIdx.x] = L.wmid[threadIdx.x] = (int)lds_off(&L.u.walk.area[0]);
   if (threadIdx.x < kWavesPerBlock) L.fdone[threadIdx.x] = L.fcount[threadIdx.x] = 0u;  // (0 is never a tag)
   if (threadIdx.x == 0) {
     L.staged = 0;
