@@ -124,6 +124,22 @@ def _stream(stream, device) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _on(stream, device):
+    """The call's stream as a context in which to allocate: memory the call
+    brings along belongs to the stream that uses it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = _stream(stream, device)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _empty(shape, dtype, device, stream):
+    with _on(stream, device):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def mas_workspace_bytes(B: int, T: int, S: int) -> int:
     return int(lib().mas_workspace_bytes(B, T, S))
 
@@ -145,7 +161,7 @@ class Workspace:
             raise ValueError(f"invalid shape B={B} T={T} S={S}")
         self.shape = (B, T, S)
         self.nbytes = n
-        self._buf = torch.empty(n + 256, dtype=torch.uint8, device=device or "cuda")
+        self._buf = _empty(n + 256, torch.uint8, device or "cuda", stream)
         off = (-self._buf.data_ptr()) % 256
         self.ptr = self._buf.data_ptr() + off
         self.device = self._buf.device
@@ -183,13 +199,13 @@ def mas_search(value, t_x, t_y, row_start_out=None, score_out=None, item_status_
     [B, T+1] int32 (see mas.h).  durations_out [B, T] int32 is optional."""
     B, T, S, pv, px, py = _batch(value, t_x, t_y)
     if row_start_out is None:
-        row_start_out = torch.empty((B, T + 1), dtype=torch.int32, device=value.device)
+        row_start_out = _empty((B, T + 1), torch.int32, value.device, stream)
     prs = _dev_ptr(row_start_out, "row_start_out", torch.int32, (B, T + 1))
     pdu = _dev_ptr(durations_out, "durations_out", torch.int32, (B, T))
     psc = _dev_ptr(score_out, "score_out", torch.float32, (B,))
     pst = _dev_ptr(item_status_out, "item_status_out", torch.int32, (B,))
     s = _stream(stream, value.device)
-    ws = _workspace(workspace, B, T, S, value.device, s)
+    ws = _workspace(workspace, B, T, S, value.device, stream)
     _check("mas_search", lib().mas_search(pv, px, py, B, T, S, prs, pdu, psc, pst, ws.ptr, ws.nbytes, s))
     return row_start_out
 
@@ -202,7 +218,7 @@ def mas_expand_path(row_start, S: int, path_out=None, stream=None):
     T = T1 - 1
     prs = _dev_ptr(row_start, "row_start", torch.int32)
     if path_out is None:
-        path_out = torch.empty((B, T, S), dtype=torch.uint8, device=row_start.device)
+        path_out = _empty((B, T, S), torch.uint8, row_start.device, stream)
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     _check("mas_expand_path", lib().mas_expand_path(prs, B, T, S, pp, _stream(stream, row_start.device)))
     return path_out
@@ -218,7 +234,7 @@ def mas_expand_text(text, row_start, S: int, out=None, stream=None):
     prs = _dev_ptr(row_start, "row_start", torch.int32, (B, T + 1))
     pt = _dev_ptr(text, "text", text.dtype)
     if out is None:
-        out = torch.empty((B, S, C), dtype=text.dtype, device=text.device)
+        out = _empty((B, S, C), text.dtype, text.device, stream)
     po = _dev_ptr(out, "out", text.dtype, (B, S, C))
     _check("mas_expand_text", lib().mas_expand_text(pt, prs, B, T, S, C, text.element_size(), po,
                                                     _stream(stream, text.device)))
@@ -240,7 +256,7 @@ def mas_loglik(mu, log_sigma, z, t_x, t_y, value_out=None, stream=None):
     px = _dev_ptr(t_x, "t_x", torch.int32, (B,))
     py = _dev_ptr(t_y, "t_y", torch.int32, (B,))
     if value_out is None:
-        value_out = torch.empty((B, T, S), dtype=torch.float32, device=mu.device)
+        value_out = _empty((B, T, S), torch.float32, mu.device, stream)
     pv = _dev_ptr(value_out, "value_out", torch.float32, (B, T, S))
     _check("mas_loglik", lib().mas_loglik(pm, pl, pz, px, py, B, T, S, D, pv, _stream(stream, mu.device)))
     return value_out
@@ -250,12 +266,12 @@ def mas_forward_ex(value, t_x, t_y, path_out=None, score_out=None, item_status_o
     """Full alignment into path_out [B, T, S] uint8 with a caller workspace."""
     B, T, S, pv, px, py = _batch(value, t_x, t_y)
     if path_out is None:
-        path_out = torch.empty((B, T, S), dtype=torch.uint8, device=value.device)
+        path_out = _empty((B, T, S), torch.uint8, value.device, stream)
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     psc = _dev_ptr(score_out, "score_out", torch.float32, (B,))
     pst = _dev_ptr(item_status_out, "item_status_out", torch.int32, (B,))
     s = _stream(stream, value.device)
-    ws = _workspace(workspace, B, T, S, value.device, s)
+    ws = _workspace(workspace, B, T, S, value.device, stream)
     _check("mas_forward_ex", lib().mas_forward_ex(pv, px, py, pp, B, T, S, psc, pst, ws.ptr, ws.nbytes, s))
     return path_out
 
@@ -266,12 +282,12 @@ def mas_forward_sentinel(value, t_x, t_y, sentinel, path_out=None, score_out=Non
     masks hold the finite negative `sentinel` (e.g. -1e9) instead of -inf."""
     B, T, S, pv, px, py = _batch(value, t_x, t_y)
     if path_out is None:
-        path_out = torch.empty((B, T, S), dtype=torch.uint8, device=value.device)
+        path_out = _empty((B, T, S), torch.uint8, value.device, stream)
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     psc = _dev_ptr(score_out, "score_out", torch.float32, (B,))
     pst = _dev_ptr(item_status_out, "item_status_out", torch.int32, (B,))
     s = _stream(stream, value.device)
-    ws = _workspace(workspace, B, T, S, value.device, s)
+    ws = _workspace(workspace, B, T, S, value.device, stream)
     _check("mas_forward_sentinel",
            lib().mas_forward_sentinel(pv, px, py, pp, B, T, S, float(sentinel), psc, pst, ws.ptr, ws.nbytes, s))
     return path_out
@@ -282,7 +298,7 @@ def mas_forward_static(value, t_x, t_y, path_out=None, score_out=None, item_stat
     workspace: allocates no device memory (see mas.h for the limit)."""
     B, T, S, pv, px, py = _batch(value, t_x, t_y)
     if path_out is None:
-        path_out = torch.empty((B, T, S), dtype=torch.uint8, device=value.device)
+        path_out = _empty((B, T, S), torch.uint8, value.device, stream)
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     psc = _dev_ptr(score_out, "score_out", torch.float32, (B,))
     pst = _dev_ptr(item_status_out, "item_status_out", torch.int32, (B,))
@@ -294,7 +310,7 @@ def mas_forward(value, t_x, t_y, path_out=None, stream=None):
     """Full alignment; the library allocates its workspace stream-ordered."""
     B, T, S, pv, px, py = _batch(value, t_x, t_y)
     if path_out is None:
-        path_out = torch.empty((B, T, S), dtype=torch.uint8, device=value.device)
+        path_out = _empty((B, T, S), torch.uint8, value.device, stream)
     pp = _dev_ptr(path_out, "path_out", torch.uint8, (B, T, S))
     _check("mas_forward", lib().mas_forward(pv, px, py, pp, B, T, S, _stream(stream, value.device)))
     return path_out
@@ -345,17 +361,6 @@ def _run_on(stream, like):
     return _stream(stream, like.device)
 
 
-def _on(stream, device):
-    """The call's stream as a context in which to allocate: memory the call
-    brings along belongs to the stream that uses it."""
-    if stream is None:
-        return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        raw = _stream(stream, device)
-        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
-    return torch.cuda.stream(stream)
-
-
 def _scratch(workspace, nbytes, like, stream):
     """(pointer, bytes) of the caller's uint8 workspace, or of a new one of
     nbytes() (0 for a shape that the call will refuse), and what keeps it alive
@@ -366,11 +371,6 @@ def _scratch(workspace, nbytes, like, stream):
     with _on(stream, like.device):
         workspace = torch.empty(n + 256, dtype=torch.uint8, device=like.device)
     return workspace.data_ptr() + -workspace.data_ptr() % 256, n, workspace
-
-
-def _empty(shape, dtype, device, stream):
-    with _on(stream, device):
-        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix):
