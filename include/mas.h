@@ -309,7 +309,9 @@ typedef struct mas_heads {
  * Precision: sums, maxima and totals in fp32.  In the 16-bit types p is rounded
  * to the type before it is multiplied, the gradients of the scores in two
  * parts (about twice the type's digits; in fp16 values below 6e-8 are lost, so
- * scale the loss); results are rounded once.  MAS_F32 multiplies in fp32.
+ * scale the loss, and values above 65504 give infinities or NaN, as the results
+ * of a loss scaled too far do); results are rounded once.  MAS_F32 multiplies in
+ * fp32.
  * A capped score errs by 2^-20 of itself at most; in the 16-bit types with caps
  * up to 256 by 2^-21 of the cap, below the rounding of p.  With larger caps they
  * run the kernels of few rows and keys at every size (slower).

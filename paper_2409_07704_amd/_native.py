@@ -317,6 +317,8 @@ def mas_forward(value, t_x, t_y, path_out=None, stream=None):
 
 
 # ------------------------------------------------ operators around the alignment
+# They take tensors as data: outputs carry no gradient, whatever their inputs
+# require; a caller runs the backward calls.
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -410,7 +412,8 @@ def mas_attention(q, k, v, t_q=None, t_k=None, causal=False, scale=None, cap=0.0
     queries are the last t_q tokens of the t_k.  causal, doc_start [B, N + 1]
     and prefix [B, N] int32: see mas.h.  lse_out [B, Hq, Tq] fp32 is what the
     backward pass takes.  workspace: a uint8 tensor of
-    mas_attention_workspace_bytes, 256-byte aligned, or None."""
+    mas_attention_workspace_bytes, 256-byte aligned, or None.  Not recorded
+    by autograd: mas_attention_backward computes the gradients."""
     d, kv = _attention_desc(q, k, t_q, t_k, causal, scale, cap, slope, doc_start, prefix)
     hq, hk, hv = _heads(q, "q", q, q.shape), _heads(k, "k", q, kv), _heads(v, "v", q, kv)
     if out is None:
@@ -466,7 +469,8 @@ def mas_qk_norm_rope(q, k, wq, wk, cos, sin, pos=None, t_x=None, eps=1e-6, inter
     head, weighted by wq, wk [D] fp32 (None: 1), and the rotation of the first
     R channels by the rows pos [B, T] int32 (None: the token's index) of cos,
     sin [P, R / 2] fp32; returns (q_out, k_out).  Padding (t >= t_x) becomes
-    zeros.  q_out, k_out may be q, k."""
+    zeros.  q_out, k_out may be q, k.  Not recorded by autograd:
+    mas_qk_norm_rope_backward computes the gradients."""
     d, ks = _qk_desc(q, k, wq, wk, cos, sin, pos, t_x, eps, interleaved)
     hq, hk = _heads(q, "q", q, q.shape), None if k is None else _heads(k, "k", q, ks)
     q_out = _empty(q.shape, q.dtype, q.device, stream) if q_out is None else q_out
@@ -519,7 +523,7 @@ def mas_align_loss(mu, log_sigma, z, row_start, item_weight=None, loss_out=None,
     T + 1] gives them, and the gradients of the items' losses, each times
     item_weight [B] (None: 1); returns (loss, dmu, dlog_sigma, dz).  dlog_sigma
     is None without log_sigma unless given; without `gradients` only those given
-    are made."""
+    are made.  Not recorded by autograd."""
     if not isinstance(mu, torch.Tensor) or mu.dim() != 3 or z.dim() != 3:
         raise ValueError("mu must be [B, T, D] and z [B, S, D]")
     B, T, D = mu.shape

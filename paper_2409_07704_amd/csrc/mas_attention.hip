@@ -29,9 +29,11 @@
 //   long forward passes: matrix and vector pipes in turn, each wave its own scores,
 //     exponents and sums, two waves a SIMD (8 items of 4096 causal frames, 16 heads of
 //     128 over 4, bf16: 643 us, 855 TFLOP/s);
-//   gradients: the vector pipe beside them (4 items, 8 heads over 2, capped, sloped:
-//     dq 325 us for 3 products of 34 GFLOP and their recomputed exponents, dk and dv
-//     527 us for 4; forward 251);
+//   gradients: no pipe alone (vector 62% and 51% busy in dq and in dk, dv, matrix 39% and
+//     30%), but the steps from scores to exponents to products in each wave and the
+//     barrier of every 64 rows or keys (4 items, 8 heads over 2, capped, sloped: dq 325 us
+//     for 3 products of 34 GFLOP and their recomputed exponents, dk and dv 527 us for 4;
+//     forward 251);
 //   short passes and documents: the chain of dependent steps from lengths to tables to
 //     tiles, about 1 us each, and few tiles behind it (64 items of up to 1001 tokens, 3
 //     heads of 64, 5 documents: 43 + 55 + 87 us for 173 MB);
@@ -1296,8 +1298,8 @@ template <class T, int DP, bool KEEP, bool EXACT> __device__ __forceinline__ voi
 // OWN: without the statistics and intervals of another kernel.
 template <class T, int DP, bool OWN, bool EXACT> __device__ __forceinline__ void few_keys(const AttnParams& p, const Place& at, FewLds<T, DP>& lds) {
   constexpr int LD = kLd<T, DP>;
-  // Products take so long in fp32 that the next tile need not be fetched meanwhile,
-  // for which there are no registers.
+  // fp32 fetches no tile ahead: with 128 channels, where the kernel spills as it is,
+  // there are no registers for one.  (Up to 96 channels it holds 244 and spills none.)
   constexpr bool kAhead = sizeof(T) == 2;
   const int b = at.pair / p.Hk, hk = at.pair % p.Hk;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;

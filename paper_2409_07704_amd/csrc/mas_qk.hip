@@ -6,8 +6,9 @@
 //   backward: dy = dz turned back, dw = sum of dy x^ over all rows,
 //   g = dy w, dx = (g - x^ mean(g x^)) / sqrt(mean(x^2) + eps).
 //
-// Bound by memory: every element is read once and written once, and nothing is
-// kept between the passes (the backward pass finds the norm again from x).  A
+// Bound by the vector pipe beside memory (78% busy forward, 80% backward: exchanges of
+// partners, conversions and selects): every element is read once and written once, and
+// nothing is kept between the passes (the backward pass finds the norm again from x).  A
 // group of lanes holds one head of one token, V neighbouring channels a lane;
 // sums over a head are exchanges inside the group, and a channel's partner in the
 // turn is in the same lane (pairs side by side) or R / 2 / V lanes away.  A group
